@@ -54,7 +54,10 @@ extern "C" {
 #endif
 
 typedef enum { COMET_D = 0, COMET_CU = 1, COMET_CN = 2, COMET_S = 3 } comet_attr_t;
-typedef enum { COMET_F64 = 0, COMET_F32 = 1 } comet_dtype_t;
+/* COMET_BF16 / COMET_F16: values of the layer operators (comet_spmm_epilogue and what follows it below) only; every other call returns
+ * COMET_ERR_UNSUPPORTED_FORMAT for them. Such a tensor is described by the caller: the level arrays of a packed tensor and a value array
+ * of its own. COMET_I32: what comet_transpose_symbolic leaves in val. */
+typedef enum { COMET_F64 = 0, COMET_F32 = 1, COMET_BF16 = 2, COMET_F16 = 3, COMET_I32 = 4 } comet_dtype_t;
 
 typedef enum {
   COMET_OK = 0,
@@ -304,6 +307,83 @@ comet_status_t comet_reorder(comet_handle_t handle, int32_t order, const int64_t
  * contractions. */
 comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor_t *A, const void *B,
                                      const int64_t *h_strides, void *out_val, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Layer operators: what a layer of a model does around a product with a sparse matrix (pruned weights times activations, a graph's
+ * adjacency matrix times features) and the gradients that training it needs. The paper has no counterpart; the products are its SpMM.
+ *
+ * Common to all of them
+ *   - Matrices are [D,CU], [CU,CU] or [CN,S]; the last two get their row boundaries from a search per row into temporary memory on
+ *     every call. Values and every dense operand have one type: COMET_F64, COMET_F32, COMET_BF16 or COMET_F16.
+ *   - fp64 sums are held in double. fp32 products are added in fp32 over at most 128 terms and those sums in double; the 16-bit
+ *     types are added in fp32. Everything between the operands and an output (bias, activation, residual) is computed in fp64 for
+ *     COMET_F64 and in fp32 otherwise, and is rounded once, when the output is stored. Results do not change from run to run.
+ *   - Only stored cells count: infinities and NaN in rows of B that a row of A does not store do not reach that row's result.
+ *   - Dense operands are row-major with any leading dimension >= R (gathered ones below 2^28 elements), aligned to one element.
+ *     16-byte aligned operands with leading dimensions that are whole multiples of 16 bytes are the fastest. Outputs must not overlap
+ *     inputs, except that `residual` may be C itself (same leading dimension).
+ *   - Asynchronous on `stream` (comet_transpose_symbolic synchronises). The handle's cached scratch is not used: temporary memory, where
+ *     a call needs any, comes from the allocator and goes back to it, in stream order, before the call returns. Calls on one
+ *     handle that overlap on the GPU, on several streams or in several captured graphs, are therefore allowed here as far as the allocator
+ *     is stream-ordered; the host side of a handle remains one call at a time. Without an allocator (cudaMalloc) calls that
+ *     need temporary memory cannot be captured: those on [CU,CU] and [CN,S] matrices, the backward passes, and products whose
+ *     matrix has more than 16,384 columns.
+ */
+typedef enum { COMET_ACT_NONE = 0, COMET_ACT_RELU = 1, COMET_ACT_GELU = 2 /* with erf */, COMET_ACT_GELU_TANH = 3, COMET_ACT_SILU = 4 } comet_act_t;
+typedef enum { COMET_BIAS_ROWS = 0, COMET_BIAS_COLS = 1 } comet_bias_t;
+
+typedef struct {
+  int32_t act;             /* comet_act_t */
+  int32_t bias_along;      /* comet_bias_t: bias[i] for every row of A, or bias[r] for every column of B */
+  const void *bias;        /* NULL: none */
+  const void *residual;    /* rows x R, leading dimension ldr; NULL: none */
+  int64_t ldr;
+  void *preact;            /* rows x R, leading dimension ldz: Z is kept here for the backward pass; NULL: not kept */
+  int64_t ldz;
+} comet_epilogue_t;
+
+/* Z = A.B + bias, C = act(Z) + residual, in one pass (comet_spmm with an epilogue). h_epilogue is HOST memory, read during the call. Rows
+ * without a stored entry give act(bias) + residual. Any R >= 1; R = 1 is the form for a single vector. act is applied to the
+ * unrounded Z. COMET_ERR_INVALID_ARG for a NULL B, C or h_epilogue, an unknown act or bias_along, a leading dimension below R. */
+comet_status_t comet_spmm_epilogue(comet_handle_t handle, const comet_sptensor_t *A, const void *B, int64_t R, int64_t ldb,
+                                   const comet_epilogue_t *h_epilogue, void *C, int64_t ldc, void *stream);
+
+/* Gradients of comet_spmm_epilogue, given dC: with dZ = dC * act'(Z), Z as the forward pass kept it (`preact`; not read for
+ * COMET_ACT_NONE, whose dZ is dC),
+ *   dval[p]  = sum_r dZ[row of p, r] B[column of p, r]     A->nnz values in A's order
+ *   dB       = A^T dZ                                      columns of A x R, leading dimension lddb, every row written
+ *   dbias    = sums of dZ along its rows or columns, by bias_along (read only where dbias is given)
+ * each only where its pointer is not NULL; the residual's gradient is dC. At: comet_transpose_symbolic(A), needed for dB alone (NULL otherwise);
+ * A's values may have changed since. B is needed for dval alone. dZ is held in the operands' type (rows x R of temporary memory). */
+comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, const comet_sptensor_t *A, const comet_sptensor_t *At, const void *B,
+                                            int64_t R, int64_t ldb, int32_t act, const void *preact, int64_t ldz, const void *dC, int64_t lddc,
+                                            int32_t bias_along, void *dbias, void *dval, void *dB, int64_t lddb, void *stream);
+
+/* Gated pair: C = act(G.B + bias_g) * (U.B + bias_u), element by element, in one pass. G and U: equal extents and type, structures of
+ * their own. bias_g, bias_u: one value per row, or NULL. preact_g, preact_u: both NULL, or both rows x R with leading dimension ldz: the
+ * two pre-activations, kept for the backward pass. */
+comet_status_t comet_spmm_gated(comet_handle_t handle, const comet_sptensor_t *G, const comet_sptensor_t *U, const void *B, int64_t R,
+                                int64_t ldb, int32_t act, const void *bias_g, const void *bias_u, void *preact_g, void *preact_u, int64_t ldz,
+                                void *C, int64_t ldc, void *stream);
+
+/* Gradients of comet_spmm_gated, given dC and the kept pre-activations: dZg = dC * Zu * act'(Zg), dZu = dC * act(Zg);
+ * dval_g, dval_u, dbias_g, dbias_u as above, dB = G^T dZg + U^T dZu; each only where its pointer is not NULL. Gt, Ut are needed for
+ * dB alone, B for dval_g and dval_u alone. */
+comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const comet_sptensor_t *G, const comet_sptensor_t *Gt,
+                                         const comet_sptensor_t *U, const comet_sptensor_t *Ut, const void *B, int64_t R, int64_t ldb,
+                                         int32_t act, const void *preact_g, const void *preact_u, int64_t ldz, const void *dC, int64_t lddc,
+                                         void *dbias_g, void *dbias_u, void *dval_g, void *dval_u, void *dB, int64_t lddb, void *stream);
+
+/* Product of two dense matrices sampled at A's stored cells: out_val[p] = sum_r P[row of p, r] Q[column of p, r]. A's values are not
+ * read (A->val must be set all the same where A has entries). P: rows of A x R, Q: columns of A x R; out_val: A->nnz values of A's type,
+ * in A's order (a value array of a tensor that shares A's levels). */
+comet_status_t comet_sddmm(comet_handle_t handle, const comet_sptensor_t *A, const void *P, int64_t ldp, const void *Q, int64_t ldq,
+                           int64_t R, void *out_val, void *stream);
+
+/* Structure of the transpose for the backward passes: the same tensor stored column by column. At is [D,CU] with A's two modes in the other
+ * order, dtype COMET_I32, and At->val holds int32 numbers: entry p of At is entry At->val[p] of A. It depends on A's structure
+ * alone, is owned by the library (comet_sptensor_free) and is accepted by the backward passes only. Synchronises `stream` as comet_pack does. */
+comet_status_t comet_transpose_symbolic(comet_handle_t handle, const comet_sptensor_t *A, void *stream, comet_sptensor_t *At);
 
 /* CSR SpMV without any allocation (the paper has no counterpart; this exists for deployment only).
  *

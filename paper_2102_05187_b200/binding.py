@@ -16,7 +16,11 @@ import torch
 D, CU, CN, S = 0, 1, 2, 3
 F64 = 0
 F32 = 1
-_TORCH_DTYPE = {F64: torch.float64, F32: torch.float32}
+BF16, F16, I32 = 2, 3, 4             # values of the layer operators; the entry numbers of transpose_symbolic
+_TORCH_DTYPE = {F64: torch.float64, F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16, I32: torch.int32}
+_VALUE_CODE = {t: c for c, t in _TORCH_DTYPE.items() if c != I32}
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
+BIAS_ROWS, BIAS_COLS = 0, 1
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -51,7 +55,8 @@ EXPORTS = [
     "comet_pack",
     "comet_sptensor_free", "comet_validate", "comet_spmv", "comet_spmm", "comet_ttv_symbolic", "comet_ttv",
     "comet_ttm_symbolic", "comet_ttm", "comet_mttkrp", "comet_spmv_static", "comet_pack_ex", "comet_ttm_symbolic_ex", "comet_reorder",
-    "comet_elementwise_mul", "comet_spmm_from_host",
+    "comet_elementwise_mul", "comet_spmm_from_host", "comet_spmm_epilogue", "comet_spmm_epilogue_backward", "comet_spmm_gated",
+    "comet_spmm_gated_backward", "comet_sddmm", "comet_transpose_symbolic",
 ]
 
 
@@ -73,6 +78,11 @@ class SpTensorStruct(C.Structure):
         ("val", C.c_void_p), ("nnz", C.c_int64),
         ("owner", C.c_void_p),
     ]
+
+
+class EpilogueStruct(C.Structure):
+    _fields_ = [("act", C.c_int32), ("bias_along", C.c_int32), ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64),
+                ("preact", C.c_void_p), ("ldz", C.c_int64)]
 
 
 _ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p)
@@ -117,6 +127,12 @@ def load_library():
     lib.comet_mttkrp.argtypes = [p, t, i32, p, p, i64, p, i64, p]
     lib.comet_pack_ex.argtypes = [p, i32, p, i64, p, p, C.c_int, p, p, C.c_uint32, p, t]
     lib.comet_sptensor_free.argtypes = [p, t, p]
+    lib.comet_spmm_epilogue.argtypes = [p, t, p, i64, i64, C.POINTER(EpilogueStruct), p, i64, p]
+    lib.comet_spmm_epilogue_backward.argtypes = [p, t, t, p, i64, i64, i32, p, i64, p, i64, i32, p, p, p, i64, p]
+    lib.comet_spmm_gated.argtypes = [p, t, t, p, i64, i64, i32, p, p, p, p, i64, p, i64, p]
+    lib.comet_spmm_gated_backward.argtypes = [p, t, t, t, t, p, i64, i64, i32, p, p, i64, p, i64, p, p, p, p, p, i64, p]
+    lib.comet_sddmm.argtypes = [p, t, p, i64, p, i64, i64, p, p]
+    lib.comet_transpose_symbolic.argtypes = [p, t, p, t]
     _lib = lib
     return lib
 
@@ -266,14 +282,27 @@ class SpTensor:
         except Exception:
             pass
 
+    def with_values(self, val: torch.Tensor) -> "SpTensor":
+        """The tensor of this one's structure (shared, and kept alive) and other values: nnz of them, float64, float32, bfloat16 or float16."""
+        _require_cuda(val)
+        if val.dtype not in _VALUE_CODE:
+            raise TypeError(f"values must be float64, float32, bfloat16 or float16, got {val.dtype}")
+        if val.numel() != self.c.nnz or not val.is_contiguous():
+            raise ValueError(f"{self.c.nnz} contiguous values are needed")
+        s = SpTensorStruct.from_buffer_copy(self.c)
+        s.val = val.data_ptr() if val.numel() else 0
+        s.dtype = _VALUE_CODE[val.dtype]
+        s.owner = None
+        return SpTensor(self.handle, s, keep=[self, val])
+
     @staticmethod
     def from_arrays(dims, mode_order, attr, pos, crd, val, handle: Handle | None = None) -> "SpTensor":
-        """Describe caller-built level arrays (torch CUDA int32 tensors, float64 or float32 values; None where a
-        level has none)."""
+        """Describe caller-built level arrays (torch CUDA int32 tensors, float64 or float32 values, or bfloat16 / float16 ones for the
+        layer operators; None where a level has none)."""
         handle = handle or default_handle()
         s = SpTensorStruct()
         order = len(dims)
-        s.order, s.dtype = order, _dtype_code(val)
+        s.order, s.dtype = order, _VALUE_CODE[val.dtype] if val.dtype in _VALUE_CODE else _dtype_code(val)
         keep = []
         for m in range(order):
             s.dims[m] = int(dims[m])
@@ -304,13 +333,16 @@ class _CudaArray:
     __slots__ = ("__cuda_array_interface__", "_owner")
 
 
-_TYPESTR = {torch.int32: ("<i4", 4), torch.float64: ("<f8", 8), torch.float32: ("<f4", 4), torch.uint8: ("|u1", 1)}
+_TYPESTR = {torch.int32: ("<i4", 4), torch.float64: ("<f8", 8), torch.float32: ("<f4", 4), torch.uint8: ("|u1", 1),
+            torch.int16: ("<i2", 2)}
 
 
 def _from_ptr(ptr, n, dtype, owner):
     """A torch tensor aliasing n elements of device memory at ptr (kept alive by `owner`)."""
     if not ptr or n == 0:
         return torch.zeros(0, dtype=dtype, device="cuda")
+    if dtype in (torch.bfloat16, torch.float16):
+        return _from_ptr(ptr, n, torch.int16, owner).view(dtype)
     typestr, itemsize = _TYPESTR[dtype]
     array = _CudaArray()
     array.__cuda_array_interface__ = {"shape": (int(n),), "typestr": typestr, "data": (int(ptr), False),
@@ -395,6 +427,183 @@ def elementwise_mul(A: SpTensor, B: torch.Tensor, out_val: torch.Tensor | None =
     s.val = out_val.data_ptr() if out_val.numel() else 0
     s.owner = None
     return SpTensor(A.handle, s, keep=[A, out_val])
+
+
+# ---- layer operators: any of the four value types, every dense operand of A's own
+
+def _rows_of(A):
+    return A.c.dims[A.c.mode_order[0]]
+
+
+def _cols_of(A):
+    return A.c.dims[A.c.mode_order[1]]
+
+
+def _operand(A, t, rows, R, what):
+    """Checks a dense operand (rows x R, or rows values where R is None) and returns its address and leading dimension."""
+    if t is None:
+        return 0, 0
+    if not t.is_cuda:
+        raise ValueError("operands must be CUDA tensors: the library has no host path")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{what} is on device {t.get_device()}, the current device is another one")
+    if t.dtype != _TORCH_DTYPE[A.c.dtype]:
+        raise TypeError(f"{what} is {t.dtype}, the sparse tensor's values are {_TORCH_DTYPE[A.c.dtype]}")
+    if R is None:
+        if t.dim() != 1 or t.shape[0] != rows or (rows > 1 and t.stride(0) != 1):
+            raise ValueError(f"{what} must be a contiguous vector of {rows} values")
+        return t.data_ptr(), 0
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != R:
+        raise ValueError(f"{what} must be {rows} x {R}, got {tuple(t.shape)}")
+    ld, step = t.stride()
+    if (step != 1 and R > 1) or (ld < R and rows > 1):
+        raise ValueError(f"{what} must be row-major")
+    return t.data_ptr(), max(ld, R)
+
+
+def _layer_matrix(*matrices):
+    for A in matrices:
+        if A.c.order != 2:
+            raise ValueError("the layer operators take matrices")
+        if A.c.dtype == I32:
+            raise TypeError("the structure of a transpose has no values")
+
+
+def transpose_symbolic(A: SpTensor) -> SpTensor:
+    """Structure of A stored column by column, for the backward passes: its `val` holds the int32 number in A of each entry."""
+    _layer_matrix(A)
+    out = SpTensorStruct()
+    st = A.handle.lib.comet_transpose_symbolic(A.handle._h, A._ref, _raw_stream(), C.byref(out))
+    A.handle.check(st, "comet_transpose_symbolic")
+    return SpTensor(A.handle, out)
+
+
+def spmm_epilogue(A: SpTensor, B: torch.Tensor, act: int = ACT_NONE, bias: torch.Tensor | None = None, bias_along: int | None = BIAS_ROWS,
+                  residual: torch.Tensor | None = None, preact: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """act(A @ B + bias) + residual in one pass; `preact` (rows x R) receives A @ B + bias for the backward pass. The bias has a value
+    per row of A (BIAS_ROWS) or per column of B (BIAS_COLS). `residual` may be `out`."""
+    _layer_matrix(A)
+    rows, R = _rows_of(A), B.shape[1]
+    b, ldb = _operand(A, B, _cols_of(A), R, "B")
+    along = BIAS_ROWS if bias is None or bias_along is None else bias_along
+    if bias is not None and bias_along is None:
+        raise ValueError("a bias needs bias_along")
+    if out is None:
+        out = B.new_empty((rows, R))
+    c, ldc = _operand(A, out, rows, R, "out")
+    e = EpilogueStruct(act, along, _operand(A, bias, rows if along == BIAS_ROWS else R, None, "bias")[0], *_operand(A, residual, rows, R, "residual"),
+                       *_operand(A, preact, rows, R, "preact"))
+    h = A.handle
+    if rows == 0:
+        return out
+    st = h.lib.comet_spmm_epilogue(h._h, A._ref, b or out.data_ptr(), R, ldb, C.byref(e), c, ldc, _raw_stream())
+    if st:
+        h.check(st, "comet_spmm_epilogue")
+    return out
+
+
+def spmm_epilogue_backward(A: SpTensor, At: SpTensor | None, B: torch.Tensor | None, dC: torch.Tensor, act: int = ACT_NONE,
+                           preact: torch.Tensor | None = None, bias_along: int | None = None, need_val: bool = True, need_dense: bool = True):
+    """Gradients (dval, dB, dbias) of spmm_epilogue; None for what is not wanted (dbias: unless `bias_along` is given). At:
+    transpose_symbolic(A), needed for dB; B is needed for dval. The residual's gradient is dC."""
+    _layer_matrix(A)
+    rows, cols, R = _rows_of(A), _cols_of(A), dC.shape[1]
+    g, lddc = _operand(A, dC, rows, R, "dC")
+    if act != ACT_NONE and preact is None:
+        raise ValueError("the activation's gradient needs preact")
+    if (need_val and B is None) or (need_dense and At is None):
+        raise ValueError("dval needs B, dB needs At")
+    z, ldz = _operand(A, preact, rows, R, "preact") if act != ACT_NONE else (0, 0)
+    b, ldb = _operand(A, B, cols, R, "B") if need_val else (0, 0)
+    dval = dC.new_empty(A.c.nnz) if need_val else None
+    dB = dC.new_empty((cols, R)) if need_dense else None
+    dbias = None if bias_along is None else dC.new_empty(rows if bias_along == BIAS_ROWS else R)
+    if rows == 0 or cols == 0:                # nothing is stored: empty or zero gradients, but for the sums of dZ
+        if rows == 0 or dbias is None:
+            return dval, None if dB is None else dB.zero_(), None if dbias is None else dbias.zero_()
+    h = A.handle
+    st = h.lib.comet_spmm_epilogue_backward(h._h, A._ref, At._ref if need_dense and cols else None, b, R, ldb, act, z, ldz, g, lddc,
+                                            0 if bias_along is None else bias_along, 0 if dbias is None else dbias.data_ptr(),
+                                            dval.data_ptr() if dval is not None and A.c.nnz else 0, 0 if dB is None or not cols else dB.data_ptr(), R,
+                                            _raw_stream())
+    if st:
+        h.check(st, "comet_spmm_epilogue_backward")
+    return dval, dB, dbias
+
+
+def _same_extents(G, U):
+    if _rows_of(G) != _rows_of(U) or _cols_of(G) != _cols_of(U) or G.c.dtype != U.c.dtype or G.handle is not U.handle:
+        raise ValueError("the two matrices must have the same extents, value type and handle")
+
+
+def spmm_gated(G: SpTensor, U: SpTensor, B: torch.Tensor, act: int = ACT_SILU, bias_g: torch.Tensor | None = None,
+               bias_u: torch.Tensor | None = None, preact=None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """act(G @ B + bias_g) * (U @ B + bias_u) in one pass; `preact`: a pair of rows x R tensors of one leading dimension that receive the
+    two pre-activations for the backward pass."""
+    _layer_matrix(G, U)
+    _same_extents(G, U)
+    rows, R = _rows_of(G), B.shape[1]
+    b, ldb = _operand(G, B, _cols_of(G), R, "B")
+    if out is None:
+        out = B.new_empty((rows, R))
+    c, ldc = _operand(G, out, rows, R, "out")
+    (zg, ldz), (zu, ldu) = [_operand(G, z, rows, R, "preact") for z in (preact if preact is not None else (None, None))]
+    if ldz != ldu:
+        raise ValueError("the two pre-activations need one leading dimension")
+    h = G.handle
+    if rows == 0:
+        return out
+    st = h.lib.comet_spmm_gated(h._h, G._ref, U._ref, b or out.data_ptr(), R, ldb, act, _operand(G, bias_g, rows, None, "bias_g")[0],
+                                _operand(G, bias_u, rows, None, "bias_u")[0], zg, zu, ldz, c, ldc, _raw_stream())
+    if st:
+        h.check(st, "comet_spmm_gated")
+    return out
+
+
+def spmm_gated_backward(G: SpTensor, Gt: SpTensor | None, U: SpTensor, Ut: SpTensor | None, B: torch.Tensor | None, dC: torch.Tensor, preact,
+                        act: int = ACT_SILU, need_val: bool = True, need_dense: bool = True, need_bias: bool = False):
+    """Gradients (dval_g, dval_u, dB, dbias_g, dbias_u) of spmm_gated; None for what is not wanted. Gt, Ut: transpose_symbolic of the two,
+    needed for dB; B is needed for the values' gradients; `preact`: the pair that the forward pass kept."""
+    _layer_matrix(G, U)
+    _same_extents(G, U)
+    rows, cols, R = _rows_of(G), _cols_of(G), dC.shape[1]
+    g, lddc = _operand(G, dC, rows, R, "dC")
+    (zg, ldz), (zu, ldu) = [_operand(G, z, rows, R, "preact") for z in preact]
+    if ldz != ldu:
+        raise ValueError("the two pre-activations need one leading dimension")
+    if (need_val and B is None) or (need_dense and (Gt is None or Ut is None)):
+        raise ValueError("the values' gradients need B, dB needs Gt and Ut")
+    b, ldb = _operand(G, B, cols, R, "B") if need_val else (0, 0)
+    dvals = [dC.new_empty(A.c.nnz) if need_val else None for A in (G, U)]
+    dB = dC.new_empty((cols, R)) if need_dense else None
+    dbias = [dC.new_empty(rows) if need_bias else None for _ in (G, U)]
+    if rows == 0:
+        return (*dvals, None if dB is None else dB.zero_(), *dbias)
+    h = G.handle
+    dense = dB is not None and cols > 0
+    st = h.lib.comet_spmm_gated_backward(h._h, G._ref, Gt._ref if dense else None, U._ref, Ut._ref if dense else None, b, R, ldb, act, zg, zu, ldz, g,
+                                         lddc, *[0 if t is None else t.data_ptr() for t in dbias],
+                                         *[t.data_ptr() if t is not None and t.numel() else 0 for t in dvals], dB.data_ptr() if dense else 0, R,
+                                         _raw_stream())
+    if st:
+        h.check(st, "comet_spmm_gated_backward")
+    return (*dvals, dB, *dbias)
+
+
+def sddmm(A: SpTensor, P: torch.Tensor, Q: torch.Tensor, out_val: torch.Tensor | None = None) -> SpTensor:
+    """P @ Q.T at A's stored cells: a tensor that shares A's level arrays (A must outlive it) and owns its values. A's values are not read."""
+    _layer_matrix(A)
+    R = P.shape[1]
+    p, ldp = _operand(A, P, _rows_of(A), R, "P")
+    q, ldq = _operand(A, Q, _cols_of(A), R, "Q")
+    if out_val is None:
+        out_val = P.new_empty(A.c.nnz)
+    o = _operand(A, out_val, A.c.nnz, None, "out_val")[0]
+    h = A.handle
+    st = h.lib.comet_sddmm(h._h, A._ref, p, ldp, q, ldq, R, o, _raw_stream())
+    if st:
+        h.check(st, "comet_sddmm")
+    return A.with_values(out_val)
 
 
 def ttv_symbolic(X: SpTensor, mode: int, out_attr=None) -> SpTensor:

@@ -23,6 +23,14 @@ comet_status_t check_tensor(const comet_sptensor_t *t, int order) {
   if (!t) return COMET_ERR_INVALID_ARG;
   if (t->order != order) return COMET_ERR_UNSUPPORTED_FORMAT;
   if (t->dtype != COMET_F64 && t->dtype != COMET_F32) return COMET_ERR_UNSUPPORTED_FORMAT;
+  return check_levels(t, order);
+}
+
+}  // namespace
+
+comet_status_t comet::check_levels(const comet_sptensor_t *t, int order) {
+  if (!t) return COMET_ERR_INVALID_ARG;
+  if (t->order != order) return COMET_ERR_UNSUPPORTED_FORMAT;
   if (t->nnz < 0) return COMET_ERR_INVALID_ARG;
   if (t->nnz > kIndexLimit) return COMET_ERR_INDEX_OVERFLOW;
   bool seen[COMET_MAX_ORDER] = {false, false, false, false};
@@ -40,6 +48,8 @@ comet_status_t check_tensor(const comet_sptensor_t *t, int order) {
   if (t->nnz > 0 && !t->val) return COMET_ERR_INVALID_ARG;
   return COMET_OK;
 }
+
+namespace {
 
 // Dense operands and outputs carry the tensor's value type and must be aligned to one element of it.
 size_t elem_size(int dtype) { return dtype == COMET_F32 ? 4 : 8; }
@@ -126,6 +136,13 @@ void *owner_alloc(Context *ctx, void *owner, size_t bytes, cudaStream_t stream) 
   return owned_alloc(ctx, static_cast<Owner *>(owner), bytes, stream);
 }
 void owner_release(Context *ctx, void *owner, cudaStream_t stream) { release(ctx, static_cast<Owner *>(owner), stream); }
+comet_status_t row_starts(Context *ctx, const comet_sptensor_t *A, int64_t rows, int32_t *pos, cudaStream_t stream) {
+  const unsigned blocks = (unsigned)ceil_div(rows + 1, 256);
+  if (A->attr[0] == COMET_CN) coo_row_pos_kernel<<<blocks, 256, 0, stream>>>(A->crd[0], A->nnz, rows, pos);
+  else expand_root_pos_kernel<<<blocks, 256, 0, stream>>>(A->crd[0], A->pos[1], A->crd_len[0], rows, pos);
+  COMET_LAUNCH_CHECK(ctx);
+  return COMET_OK;
+}
 }  // namespace comet
 
 extern "C" comet_status_t comet_sptensor_free(comet_handle_t handle, comet_sptensor_t *t, void *stream) {

@@ -117,6 +117,11 @@ void *owner_new();
 void *owner_alloc(Context *ctx, void *owner, size_t bytes, cudaStream_t stream);
 void owner_release(Context *ctx, void *owner, cudaStream_t stream);
 
+// What every entry point asks of a descriptor, its value type apart (api.cu).
+comet_status_t check_levels(const comet_sptensor_t *t, int order);
+// Row boundaries (rows + 1 words) of a [CU,CU] or sorted [CN,S] matrix.
+comet_status_t row_starts(Context *ctx, const comet_sptensor_t *A, int64_t rows, int32_t *pos, cudaStream_t stream);
+
 // Carry fix-up shared by all contraction kernels (defined in contract_vec.cu): adds the per-tile open sums
 // carry_val[tile, 0..R) onto row carry_seg[tile] of C (mapped through out_row when given); R is at most 128. cut_runs: runs
 // of very many tiles are cut; carry_seg then has carry_seg_words(num_tiles) words and the kernel that writes it clears those

@@ -1,0 +1,327 @@
+// extern "C" entry points of the layer operators: the sparse x dense product with bias, activation and residual in its epilogue, the
+// gated pair of products, their backward passes, the sampled product and the structure of the transpose.
+#include "kernels.cuh"
+#include "layer.cuh"
+
+#include <string.h>
+
+namespace comet {
+
+template <class T> comet_status_t layer_gather_typed(Context *ctx, const GatherCall &c, cudaStream_t s);   // layer_gather.cuh, a unit per type
+
+comet_status_t layer_gather(Context *ctx, int dtype, const GatherCall &c, cudaStream_t s) {
+  switch (dtype) {
+    case COMET_F64: return layer_gather_typed<double>(ctx, c, s);
+    case COMET_F32: return layer_gather_typed<float>(ctx, c, s);
+    case COMET_BF16: return layer_gather_typed<__nv_bfloat16>(ctx, c, s);
+    default: return layer_gather_typed<__half>(ctx, c, s);
+  }
+}
+
+namespace {
+
+constexpr int64_t kLdLimit = 1ll << 28;
+
+// Temporary blocks of one call, given back (in stream order) when it returns.
+struct Temps {
+  Context *ctx;
+  cudaStream_t s;
+  void *block[8];
+  int count = 0;
+  Temps(Context *c, cudaStream_t stream) : ctx(c), s(stream) {}
+  ~Temps() { for (int i = 0; i < count; ++i) ctx_free(ctx, block[i], s); }
+  void *get(size_t bytes) {
+    void *p = ctx_alloc(ctx, bytes, s);
+    if (p) block[count++] = p;
+    return p;
+  }
+};
+
+bool off_type(const void *p, size_t es) { return ((uintptr_t)p & (es - 1)) != 0; }
+
+comet_status_t check_matrix(const comet_sptensor_t *A) {
+  if (!A) return COMET_ERR_INVALID_ARG;
+  if (A->order == 2 && !layer_dtype(A->dtype)) return COMET_ERR_UNSUPPORTED_FORMAT;
+  const comet_status_t st = check_levels(A, 2);
+  if (st != COMET_OK) return st;
+  const int a0 = A->attr[0], a1 = A->attr[1];
+  if (!((a0 == COMET_D && a1 == COMET_CU) || (a0 == COMET_CU && a1 == COMET_CU) || (a0 == COMET_CN && a1 == COMET_S))) return COMET_ERR_UNSUPPORTED_FORMAT;
+  return COMET_OK;
+}
+
+int64_t row_count(const comet_sptensor_t *A) { return A->dims[A->mode_order[0]]; }
+int64_t col_count(const comet_sptensor_t *A) { return A->dims[A->mode_order[1]]; }
+
+// A by rows; [CU,CU] and [CN,S] matrices get the row boundaries that [D,CU] stores from a search per row into temporary memory.
+comet_status_t view_rows(Context *ctx, const comet_sptensor_t *A, Temps &temps, RowView *v) {
+  *v = RowView{A->pos[1], A->crd[1], A->val, row_count(A), col_count(A), A->nnz};
+  if (A->attr[0] == COMET_D) return COMET_OK;
+  int32_t *pos = (int32_t *)temps.get((size_t)(v->rows + 1) * sizeof(int32_t));
+  if (!pos) return COMET_ERR_ALLOC;
+  v->pos = pos;
+  return row_starts(ctx, A, v->rows, pos, temps.s);
+}
+
+// At as comet_transpose_symbolic makes it of A.
+comet_status_t check_transpose(const comet_sptensor_t *A, const comet_sptensor_t *At) {
+  if (!At) return COMET_ERR_INVALID_ARG;
+  const comet_status_t st = check_levels(At, 2);
+  if (st != COMET_OK) return st;
+  if (At->dtype != COMET_I32 || At->attr[0] != COMET_D || At->attr[1] != COMET_CU || At->nnz != A->nnz || At->dims[0] != A->dims[0] ||
+      At->dims[1] != A->dims[1] || At->mode_order[0] != A->mode_order[1])
+    return COMET_ERR_INVALID_ARG;
+  return COMET_OK;
+}
+
+bool good_act(int act) { return act >= COMET_ACT_NONE && act <= COMET_ACT_SILU; }
+
+// The values of A in At's order, for the gathers of a backward pass.
+comet_status_t view_transpose(Context *ctx, int dtype, const comet_sptensor_t *A, const comet_sptensor_t *At, Temps &temps, RowView *v) {
+  void *val = temps.get((size_t)A->nnz * layer_elem_size(dtype));
+  if (!val) return COMET_ERR_ALLOC;
+  *v = RowView{At->pos[1], At->crd[1], val, row_count(At), col_count(At), At->nnz};
+  return layer_pick(ctx, dtype, A->val, (const int32_t *)At->val, A->nnz, val, temps.s);
+}
+
+__global__ void entry_rows_kernel(const int32_t *__restrict__ pos, int32_t rows, int64_t n, int32_t *__restrict__ row, int32_t *__restrict__ number) {
+  const int64_t p = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (p >= n) return;
+  int32_t lo = 0, hi = rows;
+  while (hi - lo > 1) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if ((int64_t)__ldg(pos + mid) <= p) lo = mid; else hi = mid;
+  }
+  row[p] = lo;
+  number[p] = (int32_t)p;
+}
+
+}  // namespace
+}  // namespace comet
+
+using namespace comet;
+
+extern "C" comet_status_t comet_spmm_epilogue(comet_handle_t handle, const comet_sptensor_t *A, const void *B, int64_t R, int64_t ldb,
+                                              const comet_epilogue_t *h_epilogue, void *C, int64_t ldc, void *stream) {
+  if (!handle || !B || !C || !h_epilogue || R < 1 || ldb < R || ldc < R) return COMET_ERR_INVALID_ARG;
+  const comet_epilogue_t &e = *h_epilogue;
+  if (!good_act(e.act) || (e.bias_along != COMET_BIAS_ROWS && e.bias_along != COMET_BIAS_COLS)) return COMET_ERR_INVALID_ARG;
+  if ((e.residual && e.ldr < R) || (e.preact && e.ldz < R)) return COMET_ERR_INVALID_ARG;
+  comet_status_t st = check_matrix(A);
+  if (st != COMET_OK) return st;
+  const size_t es = layer_elem_size(A->dtype);
+  if (off_type(B, es) || off_type(C, es) || off_type(e.bias, es) || off_type(e.residual, es) || off_type(e.preact, es)) return COMET_ERR_MISALIGNED;
+  if (ldb >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
+  Context *ctx = reinterpret_cast<Context *>(handle);
+  cudaStream_t s = (cudaStream_t)stream;
+  Temps temps(ctx, s);
+  GatherCall c{};
+  c.mode = kLayer;
+  st = view_rows(ctx, A, temps, &c.src[0].A);
+  if (st != COMET_OK) return st;
+  c.src[0].B = B; c.src[0].ldb = ldb;
+  c.src[0].bias = e.bias;
+  c.src[0].pre = e.preact;
+  c.R = R;
+  c.act = e.act; c.bias_along = e.bias_along;
+  c.residual = e.residual; c.ldr = e.ldr; c.ldz = e.ldz;
+  c.C = C; c.ldc = ldc;
+  return layer_gather(ctx, A->dtype, c, s);
+}
+
+extern "C" comet_status_t comet_spmm_gated(comet_handle_t handle, const comet_sptensor_t *G, const comet_sptensor_t *U, const void *B, int64_t R,
+                                           int64_t ldb, int32_t act, const void *bias_g, const void *bias_u, void *preact_g, void *preact_u,
+                                           int64_t ldz, void *C, int64_t ldc, void *stream) {
+  if (!handle || !B || !C || R < 1 || ldb < R || ldc < R || !good_act(act)) return COMET_ERR_INVALID_ARG;
+  if (!preact_g != !preact_u || (preact_g && ldz < R)) return COMET_ERR_INVALID_ARG;
+  comet_status_t st = check_matrix(G);
+  if (st == COMET_OK) st = check_matrix(U);
+  if (st != COMET_OK) return st;
+  if (G->dtype != U->dtype || row_count(G) != row_count(U) || col_count(G) != col_count(U)) return COMET_ERR_INVALID_ARG;
+  const size_t es = layer_elem_size(G->dtype);
+  if (off_type(B, es) || off_type(C, es) || off_type(bias_g, es) || off_type(bias_u, es) || off_type(preact_g, es) || off_type(preact_u, es))
+    return COMET_ERR_MISALIGNED;
+  if (ldb >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
+  Context *ctx = reinterpret_cast<Context *>(handle);
+  cudaStream_t s = (cudaStream_t)stream;
+  Temps temps(ctx, s);
+  GatherCall c{};
+  c.mode = kGated;
+  st = view_rows(ctx, G, temps, &c.src[0].A);
+  if (st == COMET_OK) st = view_rows(ctx, U, temps, &c.src[1].A);
+  if (st != COMET_OK) return st;
+  for (int q = 0; q < 2; ++q) {
+    c.src[q].B = B; c.src[q].ldb = ldb;
+    c.src[q].bias = q ? bias_u : bias_g;
+    c.src[q].pre = q ? preact_u : preact_g;
+  }
+  c.R = R;
+  c.act = act; c.bias_along = COMET_BIAS_ROWS;
+  c.ldz = ldz;
+  c.C = C; c.ldc = ldc;
+  return layer_gather(ctx, G->dtype, c, s);
+}
+
+extern "C" comet_status_t comet_sddmm(comet_handle_t handle, const comet_sptensor_t *A, const void *P, int64_t ldp, const void *Q, int64_t ldq,
+                                      int64_t R, void *out_val, void *stream) {
+  if (!handle || R < 1 || ldp < R || ldq < R) return COMET_ERR_INVALID_ARG;
+  comet_status_t st = check_matrix(A);
+  if (st != COMET_OK) return st;
+  if (A->nnz > 0 && (!P || !Q || !out_val)) return COMET_ERR_INVALID_ARG;
+  const size_t es = layer_elem_size(A->dtype);
+  if (off_type(P, es) || off_type(Q, es) || off_type(out_val, es)) return COMET_ERR_MISALIGNED;
+  if (ldp >= kLdLimit || ldq >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
+  if (A->nnz == 0) return COMET_OK;
+  Context *ctx = reinterpret_cast<Context *>(handle);
+  cudaStream_t s = (cudaStream_t)stream;
+  Temps temps(ctx, s);
+  RowView v;
+  st = view_rows(ctx, A, temps, &v);
+  if (st != COMET_OK) return st;
+  return layer_sample(ctx, A->dtype, v, P, ldp, Q, ldq, R, out_val, s);
+}
+
+extern "C" comet_status_t comet_transpose_symbolic(comet_handle_t handle, const comet_sptensor_t *A, void *stream, comet_sptensor_t *At) {
+  if (!handle || !At) return COMET_ERR_INVALID_ARG;
+  if (A != At) memset(At, 0, sizeof(*At));
+  else return COMET_ERR_INVALID_ARG;
+  comet_status_t st = check_matrix(A);
+  if (st != COMET_OK) return st;
+  Context *ctx = reinterpret_cast<Context *>(handle);
+  cudaStream_t s = (cudaStream_t)stream;
+  Temps temps(ctx, s);
+  int32_t *row = (int32_t *)temps.get((size_t)A->nnz * sizeof(int32_t)), *number = (int32_t *)temps.get((size_t)A->nnz * sizeof(int32_t));
+  if (!row || !number) return COMET_ERR_ALLOC;
+  RowView v;
+  st = view_rows(ctx, A, temps, &v);
+  if (st != COMET_OK) return st;
+  if (A->nnz > 0) {
+    entry_rows_kernel<<<(unsigned)ceil_div(A->nnz, kBlockThreads), kBlockThreads, 0, s>>>(v.pos, (int32_t)v.rows, A->nnz, row, number);
+    COMET_LAUNCH_CHECK(ctx);
+  }
+  // The entry numbers ride through the packing as 32-bit values: it copies values bitwise.
+  const int32_t *coords[2];
+  coords[A->mode_order[0]] = row;
+  coords[A->mode_order[1]] = A->crd[1];
+  const int32_t order[2] = {A->mode_order[1], A->mode_order[0]}, attr[2] = {COMET_D, COMET_CU};
+  st = comet_pack(handle, 2, A->dims, A->nnz, coords, number, COMET_F32, order, attr, stream, At);
+  if (st == COMET_OK) At->dtype = COMET_I32;
+  return st;
+}
+
+extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, const comet_sptensor_t *A, const comet_sptensor_t *At, const void *B,
+                                                       int64_t R, int64_t ldb, int32_t act, const void *preact, int64_t ldz, const void *dC,
+                                                       int64_t lddc, int32_t bias_along, void *dbias, void *dval, void *dB, int64_t lddb, void *stream) {
+  if (!handle || R < 1 || !dC || lddc < R || !good_act(act)) return COMET_ERR_INVALID_ARG;
+  if (act != COMET_ACT_NONE && (!preact || ldz < R)) return COMET_ERR_INVALID_ARG;
+  if (dbias && bias_along != COMET_BIAS_ROWS && bias_along != COMET_BIAS_COLS) return COMET_ERR_INVALID_ARG;
+  if ((dval && (!B || ldb < R)) || (dB && lddb < R)) return COMET_ERR_INVALID_ARG;
+  comet_status_t st = check_matrix(A);
+  if (st != COMET_OK) return st;
+  if (dB && (st = check_transpose(A, At)) != COMET_OK) return st;
+  const size_t es = layer_elem_size(A->dtype);
+  if ((dval && off_type(B, es)) || off_type(dC, es) || off_type(dbias, es) || off_type(dval, es) || off_type(dB, es) ||
+      (act != COMET_ACT_NONE && off_type(preact, es)))
+    return COMET_ERR_MISALIGNED;
+  if ((dval && ldb >= kLdLimit) || lddc >= kLdLimit || R >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
+  Context *ctx = reinterpret_cast<Context *>(handle);
+  cudaStream_t s = (cudaStream_t)stream;
+  Temps temps(ctx, s);
+  const void *dz = dC;
+  int64_t lddz = lddc;
+  SlopeCall g{};
+  g.rows = row_count(A); g.R = R;
+  g.act = act; g.sources = 1;
+  g.dC = dC; g.lddc = lddc;
+  g.bias_along = bias_along;
+  g.bias[0] = dbias;
+  if (act != COMET_ACT_NONE) {
+    g.z[0] = preact; g.ldz = ldz;
+    if (dval || dB) {
+      g.dz[0] = temps.get((size_t)g.rows * (size_t)R * es);
+      if (!g.dz[0]) return COMET_ERR_ALLOC;
+      dz = g.dz[0];
+      lddz = R;
+    }
+  }
+  if (g.dz[0] || dbias) {
+    st = layer_slope(ctx, A->dtype, g, s);
+    if (st != COMET_OK) return st;
+  }
+  if (dval && A->nnz > 0) {
+    RowView v;
+    st = view_rows(ctx, A, temps, &v);
+    if (st == COMET_OK) st = layer_sample(ctx, A->dtype, v, dz, lddz, B, ldb, R, dval, s);
+    if (st != COMET_OK) return st;
+  }
+  if (!dB) return COMET_OK;
+  GatherCall c{};
+  c.mode = kLayer;
+  st = view_transpose(ctx, A->dtype, A, At, temps, &c.src[0].A);
+  if (st != COMET_OK) return st;
+  c.src[0].B = dz; c.src[0].ldb = lddz;
+  c.R = R;
+  c.C = dB; c.ldc = lddb;
+  return layer_gather(ctx, A->dtype, c, s);
+}
+
+extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const comet_sptensor_t *G, const comet_sptensor_t *Gt,
+                                                    const comet_sptensor_t *U, const comet_sptensor_t *Ut, const void *B, int64_t R, int64_t ldb,
+                                                    int32_t act, const void *preact_g, const void *preact_u, int64_t ldz, const void *dC,
+                                                    int64_t lddc, void *dbias_g, void *dbias_u, void *dval_g, void *dval_u, void *dB, int64_t lddb,
+                                                    void *stream) {
+  if (!handle || R < 1 || !dC || lddc < R || !preact_g || !preact_u || ldz < R || !good_act(act)) return COMET_ERR_INVALID_ARG;
+  const bool dvals = dval_g || dval_u;
+  if ((dvals && (!B || ldb < R)) || (dB && lddb < R)) return COMET_ERR_INVALID_ARG;
+  comet_status_t st = check_matrix(G);
+  if (st == COMET_OK) st = check_matrix(U);
+  if (st != COMET_OK) return st;
+  if (G->dtype != U->dtype || row_count(G) != row_count(U) || col_count(G) != col_count(U)) return COMET_ERR_INVALID_ARG;
+  if (dB) {
+    st = check_transpose(G, Gt);
+    if (st == COMET_OK) st = check_transpose(U, Ut);
+    if (st != COMET_OK) return st;
+  }
+  const size_t es = layer_elem_size(G->dtype);
+  if ((dvals && off_type(B, es)) || off_type(dC, es) || off_type(preact_g, es) || off_type(preact_u, es) || off_type(dbias_g, es) ||
+      off_type(dbias_u, es) || off_type(dval_g, es) || off_type(dval_u, es) || off_type(dB, es))
+    return COMET_ERR_MISALIGNED;
+  if ((dvals && ldb >= kLdLimit) || R >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
+  Context *ctx = reinterpret_cast<Context *>(handle);
+  cudaStream_t s = (cudaStream_t)stream;
+  Temps temps(ctx, s);
+  SlopeCall g{};
+  g.rows = row_count(G); g.R = R;
+  g.act = act; g.sources = 2;
+  g.dC = dC; g.lddc = lddc;
+  g.z[0] = preact_g; g.z[1] = preact_u; g.ldz = ldz;
+  g.bias_along = COMET_BIAS_ROWS;
+  g.bias[0] = dbias_g; g.bias[1] = dbias_u;
+  const bool need[2] = {dB || dval_g, dB || dval_u};
+  for (int q = 0; q < 2; ++q) {
+    if (!need[q]) continue;
+    g.dz[q] = temps.get((size_t)g.rows * (size_t)R * es);
+    if (!g.dz[q]) return COMET_ERR_ALLOC;
+  }
+  st = layer_slope(ctx, G->dtype, g, s);
+  if (st != COMET_OK) return st;
+  for (int q = 0; q < 2; ++q) {
+    const comet_sptensor_t *A = q ? U : G;
+    void *dval = q ? dval_u : dval_g;
+    if (!dval || A->nnz == 0) continue;
+    RowView v;
+    st = view_rows(ctx, A, temps, &v);
+    if (st == COMET_OK) st = layer_sample(ctx, G->dtype, v, g.dz[q], R, B, ldb, R, dval, s);
+    if (st != COMET_OK) return st;
+  }
+  if (!dB) return COMET_OK;
+  GatherCall c{};
+  c.mode = kSumOfTwo;
+  for (int q = 0; q < 2; ++q) {
+    st = view_transpose(ctx, G->dtype, q ? U : G, q ? Ut : Gt, temps, &c.src[q].A);
+    if (st != COMET_OK) return st;
+    c.src[q].B = g.dz[q]; c.src[q].ldb = R;
+  }
+  c.R = R;
+  c.C = dB; c.ldc = lddb;
+  return layer_gather(ctx, G->dtype, c, s);
+}
