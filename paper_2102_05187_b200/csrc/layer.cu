@@ -9,6 +9,30 @@ namespace comet {
 
 template <class T> comet_status_t layer_gather_typed(Context *ctx, const GatherCall &c, cudaStream_t s);   // layer_gather.cuh, a unit per type
 
+template <class T> comet_status_t layer_panel_typed(Context *ctx, const GatherCall &c, cudaStream_t s);    // layer_panel.cuh, likewise
+
+// A few columns of matrices whose entries are worth laying B down in every SM's shared memory: rows of B of up to 16 bytes, no more of
+// them (148 times) than the matrix has bytes, and no row more than 64 times as long as the mean.
+bool panel_fits(int dtype, const GatherCall &c) {
+  const double es = (double)layer_elem_size(dtype);
+  if ((double)c.R * es > 16.0) return false;
+  const int n = c.mode == kLayer ? 1 : 2;
+  double nnz = 0, cells = 0;
+  for (int q = 0; q < n; ++q) {
+    nnz += (double)c.src[q].A.nnz;
+    cells += (double)c.src[q].A.rows * (double)c.src[q].A.cols;
+  }
+  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz * (4 + es) >= kSmCount * (double)c.src[0].A.cols * (double)c.R * es;
+}
+comet_status_t layer_panel(Context *ctx, int dtype, const GatherCall &c, cudaStream_t s) {
+  switch (dtype) {
+    case COMET_F64: return layer_panel_typed<double>(ctx, c, s);
+    case COMET_F32: return layer_panel_typed<float>(ctx, c, s);
+    case COMET_BF16: return layer_panel_typed<__nv_bfloat16>(ctx, c, s);
+    default: return layer_panel_typed<__half>(ctx, c, s);
+  }
+}
+
 comet_status_t layer_gather(Context *ctx, int dtype, const GatherCall &c, cudaStream_t s) {
   switch (dtype) {
     case COMET_F64: return layer_gather_typed<double>(ctx, c, s);
@@ -26,7 +50,7 @@ constexpr int64_t kLdLimit = 1ll << 28;
 struct Temps {
   Context *ctx;
   cudaStream_t s;
-  void *block[8];
+  void *block[16];
   int count = 0;
   Temps(Context *c, cudaStream_t stream) : ctx(c), s(stream) {}
   ~Temps() { for (int i = 0; i < count; ++i) ctx_free(ctx, block[i], s); }
@@ -36,6 +60,54 @@ struct Temps {
     return p;
   }
 };
+
+// A dense operand of the products whose rows do not start on 16 bytes is copied into padded rows where that pays: always for the tensor-core forms,
+// which cannot do without, and for gathers of rows of several pieces where the entries gather it more than a few times over.
+// (Graph matrix of 3.2 M entries, 50 columns of fp32: the call 474 us with gathers of single values, 275 us with the copy, which is 17 of them.)
+comet_status_t pad_operand(Context *ctx, int dtype, const void *&B, int64_t &ldb, int64_t rows, int64_t R, Temps &temps) {
+  const int64_t ld = layer_padded(dtype, R);
+  void *copy = temps.get((size_t)rows * (size_t)ld * layer_elem_size(dtype));
+  if (!copy) return COMET_ERR_ALLOC;
+  const comet_status_t st = layer_pad(ctx, dtype, B, rows, R, ldb, copy, temps.s);
+  B = copy;
+  ldb = ld;
+  return st;
+}
+bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
+  return nnz >= 100000 && nnz >= 4 * rows && R * (int64_t)layer_elem_size(dtype) >= 32;
+}
+
+comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
+  if (c.src[0].A.rows == 0) return COMET_OK;
+  if (panel_fits(dtype, c)) return layer_panel(ctx, dtype, c, temps.s);
+  const bool tiles = tile_product_fits(dtype, c);
+  const int n = c.mode == kLayer ? 1 : 2;
+  for (int q = 0; q < n; ++q) {
+    GatherSource &g = c.src[q];
+    if (layer_aligned(dtype, g.B, g.ldb)) continue;
+    if (q == 1 && c.mode == kGated) {                       // one operand for both matrices
+      g.B = c.src[0].B;
+      g.ldb = c.src[0].ldb;
+      continue;
+    }
+    if (!tiles && !gathers_pay_padding(dtype, g.A.nnz, g.A.cols, c.R)) continue;
+    const comet_status_t st = pad_operand(ctx, dtype, g.B, g.ldb, g.A.cols, c.R, temps);
+    if (st != COMET_OK) return st;
+  }
+  return tiles ? tile_product(ctx, dtype, c, temps.s) : layer_gather(ctx, dtype, c, temps.s);
+}
+
+comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out, Temps &temps) {
+  const bool tiles = tile_sample_fits(dtype, A, R);
+  const bool pad_p = !layer_aligned(dtype, P, ldp), pad_q = !layer_aligned(dtype, Q, ldq);
+  if (tiles || gathers_pay_padding(dtype, A.nnz, A.rows + A.cols, R)) {
+    comet_status_t st = COMET_OK;
+    if (pad_p) st = pad_operand(ctx, dtype, P, ldp, A.rows, R, temps);
+    if (st == COMET_OK && pad_q) st = pad_operand(ctx, dtype, Q, ldq, A.cols, R, temps);
+    if (st != COMET_OK) return st;
+  }
+  return tiles ? tile_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s) : layer_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s);
+}
 
 bool off_type(const void *p, size_t es) { return ((uintptr_t)p & (es - 1)) != 0; }
 
@@ -125,7 +197,7 @@ extern "C" comet_status_t comet_spmm_epilogue(comet_handle_t handle, const comet
   c.act = e.act; c.bias_along = e.bias_along;
   c.residual = e.residual; c.ldr = e.ldr; c.ldz = e.ldz;
   c.C = C; c.ldc = ldc;
-  return layer_gather(ctx, A->dtype, c, s);
+  return product(ctx, A->dtype, c, temps);
 }
 
 extern "C" comet_status_t comet_spmm_gated(comet_handle_t handle, const comet_sptensor_t *G, const comet_sptensor_t *U, const void *B, int64_t R,
@@ -158,7 +230,7 @@ extern "C" comet_status_t comet_spmm_gated(comet_handle_t handle, const comet_sp
   c.act = act; c.bias_along = COMET_BIAS_ROWS;
   c.ldz = ldz;
   c.C = C; c.ldc = ldc;
-  return layer_gather(ctx, G->dtype, c, s);
+  return product(ctx, G->dtype, c, temps);
 }
 
 extern "C" comet_status_t comet_sddmm(comet_handle_t handle, const comet_sptensor_t *A, const void *P, int64_t ldp, const void *Q, int64_t ldq,
@@ -177,7 +249,7 @@ extern "C" comet_status_t comet_sddmm(comet_handle_t handle, const comet_sptenso
   RowView v;
   st = view_rows(ctx, A, temps, &v);
   if (st != COMET_OK) return st;
-  return layer_sample(ctx, A->dtype, v, P, ldp, Q, ldq, R, out_val, s);
+  return sampled(ctx, A->dtype, v, P, ldp, Q, ldq, R, out_val, temps);
 }
 
 extern "C" comet_status_t comet_transpose_symbolic(comet_handle_t handle, const comet_sptensor_t *A, void *stream, comet_sptensor_t *At) {
@@ -237,10 +309,11 @@ extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, co
   if (act != COMET_ACT_NONE) {
     g.z[0] = preact; g.ldz = ldz;
     if (dval || dB) {
-      g.dz[0] = temps.get((size_t)g.rows * (size_t)R * es);
+      g.lddz = layer_padded(A->dtype, R);
+      g.dz[0] = temps.get((size_t)g.rows * (size_t)g.lddz * es);
       if (!g.dz[0]) return COMET_ERR_ALLOC;
       dz = g.dz[0];
-      lddz = R;
+      lddz = g.lddz;
     }
   }
   if (g.dz[0] || dbias) {
@@ -250,7 +323,7 @@ extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, co
   if (dval && A->nnz > 0) {
     RowView v;
     st = view_rows(ctx, A, temps, &v);
-    if (st == COMET_OK) st = layer_sample(ctx, A->dtype, v, dz, lddz, B, ldb, R, dval, s);
+    if (st == COMET_OK) st = sampled(ctx, A->dtype, v, dz, lddz, B, ldb, R, dval, temps);
     if (st != COMET_OK) return st;
   }
   if (!dB) return COMET_OK;
@@ -261,7 +334,7 @@ extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, co
   c.src[0].B = dz; c.src[0].ldb = lddz;
   c.R = R;
   c.C = dB; c.ldc = lddb;
-  return layer_gather(ctx, A->dtype, c, s);
+  return product(ctx, A->dtype, c, temps);
 }
 
 extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const comet_sptensor_t *G, const comet_sptensor_t *Gt,
@@ -296,10 +369,11 @@ extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const
   g.z[0] = preact_g; g.z[1] = preact_u; g.ldz = ldz;
   g.bias_along = COMET_BIAS_ROWS;
   g.bias[0] = dbias_g; g.bias[1] = dbias_u;
+  g.lddz = layer_padded(G->dtype, R);
   const bool need[2] = {dB || dval_g, dB || dval_u};
   for (int q = 0; q < 2; ++q) {
     if (!need[q]) continue;
-    g.dz[q] = temps.get((size_t)g.rows * (size_t)R * es);
+    g.dz[q] = temps.get((size_t)g.rows * (size_t)g.lddz * es);
     if (!g.dz[q]) return COMET_ERR_ALLOC;
   }
   st = layer_slope(ctx, G->dtype, g, s);
@@ -310,7 +384,7 @@ extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const
     if (!dval || A->nnz == 0) continue;
     RowView v;
     st = view_rows(ctx, A, temps, &v);
-    if (st == COMET_OK) st = layer_sample(ctx, G->dtype, v, g.dz[q], R, B, ldb, R, dval, s);
+    if (st == COMET_OK) st = sampled(ctx, G->dtype, v, g.dz[q], g.lddz, B, ldb, R, dval, temps);
     if (st != COMET_OK) return st;
   }
   if (!dB) return COMET_OK;
@@ -319,9 +393,9 @@ extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const
   for (int q = 0; q < 2; ++q) {
     st = view_transpose(ctx, G->dtype, q ? U : G, q ? Ut : Gt, temps, &c.src[q].A);
     if (st != COMET_OK) return st;
-    c.src[q].B = g.dz[q]; c.src[q].ldb = R;
+    c.src[q].B = g.dz[q]; c.src[q].ldb = g.lddz;
   }
   c.R = R;
   c.C = dB; c.ldc = lddb;
-  return layer_gather(ctx, G->dtype, c, s);
+  return product(ctx, G->dtype, c, temps);
 }

@@ -23,8 +23,8 @@ struct RowView {
 template <class T> struct Num;
 template <> struct Num<double> { using acc = double; using sum = double; };
 template <> struct Num<float> { using acc = float; using sum = double; };
-template <> struct Num<__nv_bfloat16> { using acc = float; using sum = float; };
-template <> struct Num<__half> { using acc = float; using sum = float; };
+template <> struct Num<__nv_bfloat16> { using acc = float; using sum = float; static constexpr bool is_bf16 = true; };
+template <> struct Num<__half> { using acc = float; using sum = float; static constexpr bool is_bf16 = false; };
 
 __device__ __forceinline__ double widen(double x) { return x; }
 __device__ __forceinline__ float widen(float x) { return x; }
@@ -43,45 +43,61 @@ template <class T> struct Piece {
   __device__ __forceinline__ Piece() {}
 };
 
-// ---- activations and their slopes, in the wide type (fp32 or fp64)
-__device__ __forceinline__ float f_exp(float x) { return expf(x); }
-__device__ __forceinline__ double f_exp(double x) { return exp(x); }
+// ---- activations and their slopes, in the wide type (fp32 or fp64). Fast: for results that are rounded to 16 bits, exp and the quotient from the
+// special function unit (relative errors of 2^-21 or so).
+template <bool Fast> __device__ __forceinline__ float f_exp(float x) { return Fast ? __expf(x) : expf(x); }
+template <bool Fast> __device__ __forceinline__ double f_exp(double x) { return exp(x); }
 __device__ __forceinline__ float f_erf(float x) { return erff(x); }
 __device__ __forceinline__ double f_erf(double x) { return erf(x); }
-__device__ __forceinline__ float f_tanh(float x) { return tanhf(x); }
-__device__ __forceinline__ double f_tanh(double x) { return tanh(x); }
+template <bool Fast> __device__ __forceinline__ float f_quotient(float x, float y) { return Fast ? __fdividef(x, y) : x / y; }
+template <bool Fast> __device__ __forceinline__ double f_quotient(double x, double y) { return x / y; }
 
 constexpr double kSqrtHalf = 0.70710678118654752440, kSqrtTwoOverPi = 0.79788456080286535588, kInvSqrtTwoPi = 0.39894228040143267794;
 constexpr double kGeluCubic = 0.044715;
 
-template <class W> __device__ __forceinline__ W activate(int act, W z) {
+// 1 / (1 + exp(-x)) as (s, 1 - s), both to full relative accuracy: the exponential is taken of -|x|, which neither overflows nor cancels.
+template <bool Fast, class W> __device__ __forceinline__ void logistic(W x, W &s, W &rest) {
+  const W e = f_exp<Fast>(x > (W)0 ? -x : x), big = f_quotient<Fast>((W)1, (W)1 + e), small = e * big;
+  s = x > (W)0 ? big : small;
+  rest = x > (W)0 ? small : big;
+}
+
+template <bool Fast, class W> __device__ __forceinline__ W activate(int act, W z) {
+  W s, rest;
   switch (act) {
     case COMET_ACT_RELU: return z > (W)0 ? z : (z == z ? (W)0 : z);                   // NaN stays NaN
     case COMET_ACT_GELU: return (W)0.5 * z * ((W)1 + f_erf(z * (W)kSqrtHalf));
-    case COMET_ACT_GELU_TANH: return (W)0.5 * z * ((W)1 + f_tanh((W)kSqrtTwoOverPi * (z + (W)kGeluCubic * z * z * z)));
-    case COMET_ACT_SILU: return z / ((W)1 + f_exp(-z));
+    case COMET_ACT_GELU_TANH:                                                         // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+      logistic<Fast>((W)(2 * kSqrtTwoOverPi) * (z + (W)kGeluCubic * z * z * z), s, rest);
+      return z * s;
+    case COMET_ACT_SILU:
+      logistic<Fast>(z, s, rest);
+      return z * s;
     default: return z;
   }
 }
 
-template <class W> __device__ __forceinline__ W activate_slope(int act, W z) {
+template <bool Fast, class W> __device__ __forceinline__ W activate_slope(int act, W z) {
+  W s, rest;
   switch (act) {
     case COMET_ACT_RELU: return z > (W)0 ? (W)1 : (W)0;
-    case COMET_ACT_GELU: return (W)0.5 * ((W)1 + f_erf(z * (W)kSqrtHalf)) + z * f_exp((W)-0.5 * z * z) * (W)kInvSqrtTwoPi;
+    case COMET_ACT_GELU: return (W)0.5 * ((W)1 + f_erf(z * (W)kSqrtHalf)) + z * f_exp<Fast>((W)-0.5 * z * z) * (W)kInvSqrtTwoPi;
     case COMET_ACT_GELU_TANH: {
-      const W t = f_tanh((W)kSqrtTwoOverPi * (z + (W)kGeluCubic * z * z * z));
-      const W rise = (W)kSqrtTwoOverPi * ((W)1 + (W)(3 * kGeluCubic) * z * z);
-      return (W)0.5 * ((W)1 + t) + ((W)1 - t * t == (W)0 ? (W)0 : (W)0.5 * z * ((W)1 - t * t) * rise);
+      logistic<Fast>((W)(2 * kSqrtTwoOverPi) * (z + (W)kGeluCubic * z * z * z), s, rest);
+      const W bend = s * rest;
+      return s + (bend == (W)0 ? (W)0 : z * bend * (W)(2 * kSqrtTwoOverPi) * ((W)1 + (W)(3 * kGeluCubic) * z * z));
     }
-    case COMET_ACT_SILU: {
-      const W g = (W)1 / ((W)1 + f_exp(-z));
-      return g * ((W)1 + z * ((W)1 - g));
-    }
+    case COMET_ACT_SILU:
+      logistic<Fast>(z, s, rest);
+      return s * ((W)1 + z * rest);
     default: return (W)1;
   }
 }
 
 // ---- launchers
+inline size_t layer_elem_size(int dtype) { return dtype == COMET_F64 ? 8 : dtype == COMET_F32 ? 4 : 2; }
+inline bool layer_dtype(int dtype) { return dtype >= COMET_F64 && dtype <= COMET_F16; }
+inline bool layer_aligned(int dtype, const void *p, int64_t ld) { return !p || (((uintptr_t)p & 15) == 0 && ld * (int64_t)layer_elem_size(dtype) % 16 == 0); }
 
 // One of the up to two products of a call: its matrix, its dense operand, and, for its own pre-activation, bias and place to keep it.
 struct GatherSource {
@@ -108,8 +124,16 @@ comet_status_t layer_gather(Context *ctx, int dtype, const GatherCall &call, cud
 comet_status_t layer_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R,
                             void *out, cudaStream_t s);
 
+// The same two on the tensor cores (layer_tile_product.cu, layer_tile_sample.cu), and whether a call is one for them.
+bool tile_product_fits(int dtype, const GatherCall &call);
+comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &call, cudaStream_t s);
+// (These two want dense operands that start on 16 bytes with rows that are a whole number of 16 bytes apart.)
+bool tile_sample_fits(int dtype, const RowView &A, int64_t R);
+comet_status_t tile_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out,
+                           cudaStream_t s);
+
 // Gradients of the pre-activations and of the biases. One source: dz0 = dC * f'(z0). Two: dz0 = dC * z1 * f'(z0), dz1 = dC * f(z0).
-// dz* (rows x R, contiguous) and bias* may be NULL.
+// dz* (rows x R, leading dimension lddz) and bias* may be NULL.
 struct SlopeCall {
   int64_t rows, R;
   int act, bias_along, sources;
@@ -118,13 +142,20 @@ struct SlopeCall {
   const void *z[2];
   int64_t ldz;
   void *dz[2], *bias[2];
+  int64_t lddz;
 };
 comet_status_t layer_slope(Context *ctx, int dtype, const SlopeCall &call, cudaStream_t s);
+
+// A copy of a rows x R matrix with rows layer_padded values apart (the padding is not written): a whole number of 16 bytes, of 128 where the
+// tensor-core forms take 16-bit rows of 64 values and more (a tile's row is then one line).
+inline int64_t layer_padded(int dtype, int64_t R) {
+  const int64_t v = dtype == COMET_F64 ? 2 : dtype == COMET_F32 ? 4 : R > 32 ? 64 : 8;
+  return (R + v - 1) / v * v;
+}
+comet_status_t layer_pad(Context *ctx, int dtype, const void *in, int64_t rows, int64_t R, int64_t ld, void *out, cudaStream_t s);
 
 // out[p] = val[index[p]] for the transposed matrix's entries
 comet_status_t layer_pick(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, void *out, cudaStream_t s);
 
-inline size_t layer_elem_size(int dtype) { return dtype == COMET_F64 ? 8 : dtype == COMET_F32 ? 4 : 2; }
-inline bool layer_dtype(int dtype) { return dtype >= COMET_F64 && dtype <= COMET_F16; }
 
 }  // namespace comet

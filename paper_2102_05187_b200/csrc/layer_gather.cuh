@@ -155,7 +155,7 @@ __device__ __forceinline__ void finish_row(const GatherArgs<T> &a, int64_t i, co
         else a.src[q].pre[i * a.ldz + col] = narrow<T, acc_t>(z[q]);
       }
     }
-    acc_t y = activate(a.act, z[0]);
+    acc_t y = activate<sizeof(T) == 2>(a.act, z[0]);
     if (NACC == 2) y *= z[NACC - 1];
     if (a.res) y += widen(vec ? res.at[VEC ? v : 0] : a.res[i * a.ldr + col]);
     out[v] = y;

@@ -19,17 +19,17 @@ template <class T> struct SlopeArgs {
   const T *dC, *z[2];
   T *dz[2];
   T *row_bias[2];
-  int64_t rows, R, lddc, ldz;
+  int64_t rows, R, lddc, ldz, lddz;
   int act, sources;
 };
 
 template <class T> __device__ __forceinline__ void slopes(const SlopeArgs<T> &a, typename Num<T>::acc g, typename Num<T>::acc z0, typename Num<T>::acc z1,
                                                           typename Num<T>::acc (&d)[2]) {
   if (a.sources == 1) {
-    d[0] = a.act == COMET_ACT_NONE ? g : g * activate_slope(a.act, z0);
+    d[0] = a.act == COMET_ACT_NONE ? g : g * activate_slope<sizeof(T) == 2>(a.act, z0);
   } else {
-    d[0] = a.act == COMET_ACT_NONE ? g * z1 : g * z1 * activate_slope(a.act, z0);
-    d[1] = g * activate(a.act, z0);
+    d[0] = a.act == COMET_ACT_NONE ? g * z1 : g * z1 * activate_slope<sizeof(T) == 2>(a.act, z0);
+    d[1] = g * activate<sizeof(T) == 2>(a.act, z0);
   }
 }
 
@@ -72,7 +72,7 @@ template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer
         if (q >= a.sources) continue;
         sum[q] += (double)part[q];
         if (!a.dz[q]) continue;
-        T *to = a.dz[q] + i * a.R + col;
+        T *to = a.dz[q] + i * a.lddz + col;
         if (full) *reinterpret_cast<uint4 *>(to) = out[q].raw;
         else {
 #pragma unroll
@@ -132,7 +132,7 @@ template <class T> __global__ void __launch_bounds__(kSlopeThreads) column_join_
 template <class T> comet_status_t slope_typed(Context *ctx, const SlopeCall &c, cudaStream_t s) {
   SlopeArgs<T> a{};
   a.dC = (const T *)c.dC;
-  a.rows = c.rows; a.R = c.R; a.lddc = c.lddc; a.ldz = c.ldz;
+  a.rows = c.rows; a.R = c.R; a.lddc = c.lddc; a.ldz = c.ldz; a.lddz = c.lddz;
   a.act = c.act; a.sources = c.sources;
   constexpr int V = 16 / sizeof(T);
   const auto ok = [](const void *p, int64_t ld) { return !p || (((uintptr_t)p & 15) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0); };
@@ -141,7 +141,7 @@ template <class T> comet_status_t slope_typed(Context *ctx, const SlopeCall &c, 
     a.z[q] = (const T *)c.z[q];
     a.dz[q] = (T *)c.dz[q];
     if (c.bias_along == COMET_BIAS_ROWS) a.row_bias[q] = (T *)c.bias[q];
-    vec = vec && ok(c.z[q], c.ldz) && ok(c.dz[q], c.R);
+    vec = vec && ok(c.z[q], c.ldz) && ok(c.dz[q], c.lddz);
     rows_pass = rows_pass || a.dz[q] || a.row_bias[q];
   }
   if (rows_pass) {
@@ -182,7 +182,35 @@ template <class V> __global__ void __launch_bounds__(kBlockThreads) layer_pick_k
   if (p < n) out[p] = __ldg(val + ld_stream(index + p));
 }
 
+// A warp per row and run of 1,024 values.
+template <class V> __global__ void __launch_bounds__(kBlockThreads) layer_pad_kernel(const V *__restrict__ in, int64_t rows, int64_t R, int64_t ld, int64_t ldo,
+                                                                                     V *__restrict__ out) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i = (int64_t)blockIdx.x * (kBlockThreads / 32) + (threadIdx.x >> 5);
+  if (i >= rows) return;
+  for (int64_t first = (int64_t)blockIdx.y * 1024; first < R; first += (int64_t)gridDim.y * 1024) {
+    const V *from = in + i * ld;
+    V *to = out + i * ldo;
+#pragma unroll 8
+    for (int64_t col = first + lane; col < min(R, first + 1024); col += 32) to[col] = __ldg(from + col);
+  }
+}
+
 }  // namespace
+
+comet_status_t layer_pad(Context *ctx, int dtype, const void *in, int64_t rows, int64_t R, int64_t ld, void *out, cudaStream_t s) {
+  if (rows == 0) return COMET_OK;
+  const int64_t runs = ceil_div(R, 1024);
+  const dim3 grid((unsigned)ceil_div(rows, kBlockThreads / 32), (unsigned)(runs < 65535 ? runs : 65535));
+  const int64_t ldo = layer_padded(dtype, R);
+  switch (layer_elem_size(dtype)) {
+    case 8: layer_pad_kernel<<<grid, kBlockThreads, 0, s>>>((const unsigned long long *)in, rows, R, ld, ldo, (unsigned long long *)out); break;
+    case 4: layer_pad_kernel<<<grid, kBlockThreads, 0, s>>>((const unsigned int *)in, rows, R, ld, ldo, (unsigned int *)out); break;
+    default: layer_pad_kernel<<<grid, kBlockThreads, 0, s>>>((const unsigned short *)in, rows, R, ld, ldo, (unsigned short *)out);
+  }
+  COMET_LAUNCH_CHECK(ctx);
+  return COMET_OK;
+}
 
 comet_status_t layer_slope(Context *ctx, int dtype, const SlopeCall &c, cudaStream_t s) {
   if (c.rows == 0) {                                       // no row: a column's sum is empty

@@ -1,0 +1,180 @@
+// The sampled product on the tensor cores: 16-bit values and matrices whose cells are stored densely enough that computing the whole block
+// P[128 rows] Q[N rows]^T and keeping the stored cells of it costs less than a dot product per cell.
+//
+// A CTA of ten warps: one thread copies tiles of P and Q (64 values of k, by tensor map, zeros outside), one issues the products, and
+// eight warps meanwhile look up where each of the 128 rows' entries enter and leave the block's columns; then they move the block from tensor memory to
+// shared memory and write the stored cells of it, a warp per row, entries in order.
+#include "layer_tile.cuh"
+
+namespace comet {
+namespace {
+
+constexpr int kRows = 128, kK = 64, kWarps = 10;
+constexpr int kStages = 4;
+
+template <class T> struct SampleTileArgs {
+  const int32_t *pos, *crd;
+  T *out;
+  int32_t rows, cols, k_blocks, n;
+  int32_t *status;
+};
+
+template <class T>
+__global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
+                                                                     const SampleTileArgs<T> a) {
+  extern __shared__ char raw_smem[];
+  __shared__ uint64_t bars[2 * kStages + 1];
+  __shared__ uint32_t tmem_at;
+  __shared__ int failed;
+  __shared__ int32_t first[kRows], last[kRows];
+  char *smem = reinterpret_cast<char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = a.n;
+  const int stage_bytes = (kRows + n) * kK * 2;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = full + 16 * kStages;
+  const int32_t row0 = (int32_t)blockIdx.x * kRows, col0 = (int32_t)blockIdx.y * n;
+  uint32_t columns = 32;
+  while (columns < (uint32_t)n) columns <<= 1;
+  if (threadIdx.x == 0) {
+    failed = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(full + 8 * s, 1);
+      bar_init(empty + 8 * s, 1);
+    }
+    bar_init(done, 1);
+    fence_bar_init();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_at), columns);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t d = tmem_at;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int32_t t = 0; t < a.k_blocks; ++t) {
+        const int s = t % kStages, round = t / kStages;
+        if (round > 0 && !bar_wait(empty + 8 * s, (round - 1) & 1, &failed)) break;
+        const uint32_t p = smem_u32(smem + s * stage_bytes);
+        bar_expect(full + 8 * s, (uint32_t)stage_bytes);
+        copy_box(p, &map_p, t * kK, row0, full + 8 * s);
+        copy_box(p + kRows * kK * 2, &map_q, t * kK, col0, full + 8 * s);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t kind = product_kind(Num<T>::is_bf16, false, kRows, n);
+      for (int32_t t = 0; t < a.k_blocks; ++t) {
+        const int s = t % kStages, round = t / kStages;
+        if (!bar_wait(full + 8 * s, round & 1, &failed)) break;
+        tc_fence_after();
+        const uint32_t p = smem_u32(smem + s * stage_bytes);
+        const uint64_t x = operand_at(p, 16, 1024), y = operand_at(p + kRows * kK * 2, 16, 1024);
+#pragma unroll
+        for (int k = 0; k < kK / 16; ++k) tc_product(d, x + k * 2, y + k * 2, kind, t > 0 || k > 0);
+        tc_commit(empty + 8 * s);
+      }
+      tc_commit(done);
+    }
+  } else {
+    // where each row's entries enter the block's columns (threads 64..191) and leave them (192..319)
+    const int k = (int)threadIdx.x - 64, r = k & (kRows - 1);
+    const int32_t i = row0 + r;
+    int32_t lo = 0, hi = 0;
+    if (i < a.rows) { lo = __ldg(a.pos + i); hi = __ldg(a.pos + i + 1); }
+    const int32_t limit = k < kRows ? col0 : (int32_t)min((int64_t)a.cols, (int64_t)col0 + n);
+    while (lo < hi) {
+      const int32_t mid = lo + (hi - lo) / 2;
+      if (__ldg(a.crd + mid) < limit) lo = mid + 1; else hi = mid;
+    }
+    (k < kRows ? first : last)[r] = lo;
+  }
+
+  __syncwarp();
+  const bool ok = bar_wait_warp(done, 0, &failed) && !__any_sync(0xffffffffu, failed);
+  tc_fence_after();
+  float *block = reinterpret_cast<float *>(smem);      // [n][kRows + 1]: the stages are free
+  if (warp >= 2 && ok) {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    for (int c = half * 16; c < n; c += 32) {
+      float x[16];
+      tmem_load16(d + ((uint32_t)(quarter * 32) << 16) + c, x);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) block[(c + v) * (kRows + 1) + quarter * 32 + lane] = x[v];
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp >= 2 && ok) {
+    for (int r = warp - 2; r < kRows; r += kWarps - 2) {
+      const int32_t to = last[r];
+      for (int32_t p = first[r] + lane; p < to; p += 32) {
+        const uint32_t c = min((uint32_t)(__ldg(a.crd + p) - col0), (uint32_t)n - 1u);
+        a.out[p] = narrow<T, float>(block[c * (kRows + 1) + r]);
+      }
+    }
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free(d, columns);
+  }
+  if (threadIdx.x == 0 && failed) give_up(full, kStages, a.status);
+}
+
+template <class T>
+comet_status_t sample_tiles(Context *ctx, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out, cudaStream_t s) {
+  SampleTileArgs<T> a{};
+  a.pos = A.pos; a.crd = A.crd;
+  a.out = (T *)out;
+  a.rows = (int32_t)A.rows; a.cols = (int32_t)A.cols;
+  a.k_blocks = (int32_t)ceil_div(R, kK);
+  const int64_t groups = ceil_div(A.cols, 64), tiles = ceil_div(groups, 4);
+  a.n = (int)(ceil_div(groups, tiles) * 64);
+  a.status = ctx->h_pinned + kTileStatusWord;
+  CUtensorMap mp, mq;
+  if (!tile_map(&mp, Num<T>::is_bf16, P, A.rows, R, ldp, kRows) || !tile_map(&mq, Num<T>::is_bf16, Q, A.cols, R, ldq, a.n)) return COMET_ERR_CUDA;
+  const size_t ring = (size_t)kStages * (kRows + a.n) * kK * 2, block = (size_t)a.n * (kRows + 1) * sizeof(float);
+  const size_t bytes = (ring > block ? ring : block) + 1024;
+  auto *kernel = tile_sample_kernel<T>;
+  COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  kernel<<<dim3((unsigned)ceil_div(A.rows, kRows), (unsigned)tiles), kWarps * 32, bytes, s>>>(mp, mq, a);
+  COMET_LAUNCH_CHECK(ctx);
+  return COMET_OK;
+}
+
+}  // namespace
+
+bool tile_sample_fits(int dtype, const RowView &A, int64_t R) {
+  if (dtype != COMET_BF16 && dtype != COMET_F16) return false;
+  if (R < 8 || R >= (1ll << 24)) return false;
+  return (double)A.nnz * 64 >= (double)A.rows * (double)A.cols && A.cols < 65535ll * 64;
+}
+
+comet_status_t tile_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out,
+                           cudaStream_t s) {
+  const comet_status_t st = tile_status(ctx);
+  if (st != COMET_OK) return st;
+  return dtype == COMET_BF16 ? sample_tiles<__nv_bfloat16>(ctx, A, P, ldp, Q, ldq, R, out, s) : sample_tiles<__half>(ctx, A, P, ldp, Q, ldq, R, out, s);
+}
+
+// ---- tensor maps
+// The driver's encoder, found through the runtime (nothing links against libcuda).
+bool tile_map(CUtensorMap *map, bool bf16, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static Encode encode = [] {
+    void *f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(base), dims, strides, box, steps,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace comet
