@@ -5,7 +5,7 @@
 // touch up to 32 lines, a line a cycle (35 us for one token through a gated pair of 13 M entries, whose bytes take 12). So B, padded to V values a
 // row, is laid down in shared memory, as many rows at a time as fit (a panel), where 32 arbitrary rows cost the bank conflicts alone. One CTA
 // of 32 warps per SM owns a stretch of rows; `parts` warps share a row, each with a contiguous part of its entries, 8 entries a lane and
-// round, the next round's in flight meanwhile. A part stops where its columns leave the panel and goes on from there with the
+// round (4 of fp64), the next round's in flight meanwhile. A part stops where its columns leave the panel and goes on from there with the
 // next one. The parts' sums meet in shared memory and are added in their order.
 #pragma once
 
@@ -23,37 +23,44 @@ template <class T> struct PanelArgs {
   int64_t ldc, ldr, ldz;
   T *C;
   const T *res;
-  int32_t rows, cols, panel_rows, panels, parts;
+  int32_t rows, cols, panel_rows, panels, parts, log_parts;
   int R, act, bias_along, nsrc;
 };
 
+constexpr int32_t kNoColumn = 2147483647;
+
+// Entries of one lane in a round: kE fours, 128 entries apart.
 template <class T> struct Round {
-  int32_t c[8];                                // -1: none
-  T v[8];
-  // entries base + 4 * (32 * e + lane) .. + 3, e = 0, 1, as far as they lie in [from, end)
-  __device__ __forceinline__ void read(const int32_t *__restrict__ crd, const T *__restrict__ val, int64_t base, int32_t from, int32_t end, bool aligned) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int64_t i = base + 4 * (32 * e + lane);
-      if (aligned && i >= from && i + 4 <= end) {
-        const int4 x = __ldcs(reinterpret_cast<const int4 *>(crd + i));
-        c[4 * e] = x.x; c[4 * e + 1] = x.y; c[4 * e + 2] = x.z; c[4 * e + 3] = x.w;
-        if (sizeof(T) == 2) {
-          const uint2 y = __ldcs(reinterpret_cast<const uint2 *>(val + i));
-          *reinterpret_cast<uint2 *>(v + 4 * e) = y;
-        } else {
-#pragma unroll
-          for (int k = 0; k < (int)sizeof(T) / 4; ++k)
-            reinterpret_cast<uint4 *>(v + 4 * e)[k] = __ldcs(reinterpret_cast<const uint4 *>(val + i) + k);
-        }
+  static constexpr int kE = sizeof(T) == 8 ? 1 : 2, kEntries = 128 * kE;
+  int32_t c[4 * kE];
+  T v[4 * kE];
+  __device__ __forceinline__ void read4(const int32_t *__restrict__ crd, const T *__restrict__ val, int32_t i, int e, bool aligned) {
+    if (aligned) {
+      const int4 x = __ldcs(reinterpret_cast<const int4 *>(crd + i));
+      c[4 * e] = x.x; c[4 * e + 1] = x.y; c[4 * e + 2] = x.z; c[4 * e + 3] = x.w;
+      if (sizeof(T) == 2) {
+        *reinterpret_cast<uint2 *>(v + 4 * e) = __ldcs(reinterpret_cast<const uint2 *>(val + i));
       } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const bool have = i + k >= from && i + k < end;
-          c[4 * e + k] = have ? __ldg(crd + i + k) : -1;
-          v[4 * e + k] = have ? val[i + k] : (T)0.0f;
-        }
+        for (int k = 0; k < (int)sizeof(T) / 4; ++k) reinterpret_cast<uint4 *>(v + 4 * e)[k] = __ldcs(reinterpret_cast<const uint4 *>(val + i) + k);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        c[4 * e + k] = __ldg(crd + i + k);
+        v[4 * e + k] = val[i + k];
+      }
+    }
+  }
+  // i: the lane's first entry; fours that do not begin before `end` (a multiple of 4) get the column `none` and zeros
+  __device__ __forceinline__ void read(const typename PanelArgs<T>::Source &s, int32_t i, int32_t end, int32_t none) {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      if (i + 128 * e < end) {
+        read4(s.crd, s.val, i + 128 * e, e, s.aligned);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { c[4 * e + k] = none; v[4 * e + k] = (T)0.0f; }
       }
     }
   }
@@ -61,13 +68,100 @@ template <class T> struct Round {
 
 template <class T, int V> struct alignas(sizeof(T) * V) Few { T at[V]; };
 
-template <class T, int V, int NACC>
+// A row part: which one, and its entries.
+struct Part {
+  int q, unit;
+  int32_t from, end;
+  // This lane's first entry among the fours (they start on multiples of 4), and how many entries of fours there are.
+  __device__ __forceinline__ void split(int32_t &i, int32_t &left) const {
+    const int32_t first = min(end, (from + 3) & ~3), last = max(first, end & ~3);
+    i = first + 4 * (threadIdx.x & 31);
+    left = last - first;
+  }
+};
+// The up to three entries in front of a part's first four and behind its last one: a lane each.
+template <class T> struct Single {
+  int32_t c, at;
+  T v;
+  __device__ __forceinline__ void read(const typename PanelArgs<T>::Source &s, const Part &w, int32_t none) {
+    const int lane = threadIdx.x & 31;
+    const int32_t first = min(w.end, (w.from + 3) & ~3), last = max(first, w.end & ~3);
+    at = lane < 4 ? w.from + lane : last + lane - 4;
+    const bool have = lane < 4 ? at < first : lane < 8 && at < w.end;
+    c = have ? __ldg(s.crd + at) : none;
+    v = have ? s.val[at] : (T)0.0f;
+  }
+};
+
+// One part's sums over its entries, as far as their columns lie in the panel [c0, c1). Returns the first entry beyond the panel, or the part's end.
+// `several`: there are more panels than this one. Behind the panel's rows lies one of zeros: entries that are none of the panel's are
+// multiplied by it, with a weight of zero, so that the sums need no branches.
+template <class T, int V, bool several>
+__device__ __forceinline__ int32_t part_sum(const typename PanelArgs<T>::Source &s, const Part &part, int32_t c0, int32_t c1, const Few<T, V> *panel,
+                                            typename Num<T>::sum (&sum)[V]) {
+  using acc_t = typename Num<T>::acc;
+  constexpr int kStep = Round<T>::kEntries;
+  const int32_t none = several ? kNoColumn : c1;
+  const Few<T, V> *at = panel - c0;
+  uint32_t beyond = 0xffffffffu;                                 // this lane's first entry beyond the panel
+  bool going = true;
+  const auto use = [&](const Round<T> &r, int32_t i) {
+    acc_t acc[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] = (acc_t)0;
+#pragma unroll
+    for (int e = 0; e < 4 * Round<T>::kE; ++e) {
+      const Few<T, V> x = at[several ? min(r.c[e], c1) : r.c[e]];
+      const acc_t w = !several || r.c[e] < c1 ? widen(r.v[e]) : (acc_t)0;
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[k] += w * widen(x.at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum[k] += acc[k];
+    if (several && __shfl_sync(0xffffffffu, r.c[4 * Round<T>::kE - 1], 31) >= c1) {
+#pragma unroll
+      for (int e = 4 * Round<T>::kE - 1; e >= 0; --e)
+        if (r.c[e] >= c1 && r.c[e] != kNoColumn) beyond = (uint32_t)(i + 128 * (e >> 2) + (e & 3));
+      going = !__any_sync(0xffffffffu, beyond != 0xffffffffu);
+    }
+  };
+  Single<T> one;
+  one.read(s, part, none);
+  int32_t i, left;
+  part.split(i, left);
+  const int32_t last = i + left - 4 * (int32_t)(threadIdx.x & 31);
+  Round<T> x, y;
+  x.read(s, i, last, none);
+  while (left > 0) {
+    if (left > kStep) y.read(s, i + kStep, last, none);
+    use(x, i);
+    i += kStep;
+    left -= kStep;
+    if (left <= 0 || !going) break;
+    if (left > kStep) x.read(s, i + kStep, last, none);
+    use(y, i);
+    i += kStep;
+    left -= kStep;
+    if (!going) break;
+  }
+  if (one.c < c1) {
+    const Few<T, V> b = at[one.c];
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum[k] += widen(one.v) * widen(b.at[k]);
+  } else if (several && one.c != kNoColumn) {
+    beyond = min(beyond, (uint32_t)one.at);
+  }
+  return several ? (int32_t)min((uint32_t)part.end, __reduce_min_sync(0xffffffffu, beyond)) : part.end;
+}
+
+template <class T, int V, int NACC, bool several>
 __global__ void __launch_bounds__(kPanelThreads, 1) layer_panel_kernel(const PanelArgs<T> a) {
   using acc_t = typename Num<T>::acc;
   using sum_t = typename Num<T>::sum;
   extern __shared__ __align__(16) char smem[];
   __shared__ sum_t sums[NACC][kPanelUnits][V];
-  __shared__ int32_t reached[NACC == 2 ? 2 : 1][kPanelUnits];            // where a part goes on (one source at a time, or the pair's two)
+  __shared__ int32_t reached[NACC][kPanelUnits];                         // where a part goes on (one source at a time, or the pair's two)
+  __shared__ int32_t bounds[2][kPanelUnits + 1];                         // of the rows at hand
   Few<T, V> *panel = reinterpret_cast<Few<T, V> *>(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int32_t row_begin = (int32_t)((int64_t)a.rows * blockIdx.x / gridDim.x), row_end = (int32_t)((int64_t)a.rows * (blockIdx.x + 1) / gridDim.x);
@@ -77,6 +171,8 @@ __global__ void __launch_bounds__(kPanelThreads, 1) layer_panel_kernel(const Pan
   for (int32_t row0 = row_begin; row0 < row_end; row0 += rows_at_once) {
     const int32_t rows = min(rows_at_once, row_end - row0), units = rows * a.parts;
     for (int k = threadIdx.x; k < NACC * units * V; k += kPanelThreads) (&sums[0][0][0])[(k / (units * V)) * (kPanelUnits * V) + k % (units * V)] = (sum_t)0;
+    for (int q = 0; q < a.nsrc; ++q)
+      for (int k = threadIdx.x; k <= rows; k += kPanelThreads) bounds[q][k] = __ldg(a.src[q].pos + row0 + k);
     for (int pass = 0; pass < passes; ++pass) {
       for (int32_t p = 0; p < a.panels; ++p) {
         const int32_t c0 = p * a.panel_rows, c1 = min(a.cols, c0 + a.panel_rows);
@@ -97,61 +193,41 @@ __global__ void __launch_bounds__(kPanelThreads, 1) layer_panel_kernel(const Pan
               reinterpret_cast<T *>(smem)[k] = r < a.R ? B[(int64_t)(c0 + j) * ldb + r] : (T)0.0f;
             }
           }
+          if (threadIdx.x < V) reinterpret_cast<T *>(smem)[(c1 - c0) * V + threadIdx.x] = (T)0.0f;
           __syncthreads();
         }
-        for (int u = warp; u < units * NACC; u += kPanelWarps) {
-          const int q = NACC == 2 ? u % 2 : 0, unit = NACC == 2 ? u / 2 : u;
-          const typename PanelArgs<T>::Source &s = a.src[NACC == 2 ? q : pass];
-          const int32_t row = row0 + unit / a.parts, part = unit % a.parts;
-          const int32_t b = __ldg(s.pos + row), n = __ldg(s.pos + row + 1) - b;
-          // parts begin on multiples of 4 entries
-          const int32_t share = (n / a.parts + 4) & ~3;
-          const int32_t mine = (int32_t)min((int64_t)n, (int64_t)part * share), end = b + (int32_t)min((int64_t)n, (int64_t)(part + 1) * share);
-          int32_t from = b + mine;
-          if (p > 0) from = reached[q][unit];
-          acc_t acc[V];
-          sum_t sum[V];
-#pragma unroll
-          for (int v = 0; v < V; ++v) sum[v] = (sum_t)0;
-          int64_t base = from & ~3;
-          Round<T> now, next;
-          int32_t stop = end;
-          now.read(s.crd, s.val, base, from, end, s.aligned);
-          while (base < stop) {
-            next.read(s.crd, s.val, base + 256, from, end, s.aligned);
-#pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] = (acc_t)0;
-            int32_t left = -1;                                            // this lane's first entry beyond the panel
-#pragma unroll
-            for (int e = 7; e >= 0; --e) {
-              const uint32_t j = (uint32_t)(now.c[e] - c0);
-              if (j < (uint32_t)(c1 - c0)) {
-                const Few<T, V> x = panel[j];
-                const acc_t w = widen(now.v[e]);
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[v] += w * widen(x.at[v]);
-              } else if (now.c[e] >= c1) {
-                left = (int32_t)(base + 4 * (32 * (e >> 2) + lane) + (e & 3));
-              }
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum[v] += acc[v];
-            if (a.panels > 1) {
-              const uint32_t nearest = __reduce_min_sync(0xffffffffu, (uint32_t)left);
-              if (nearest != 0xffffffffu) { stop = (int32_t)nearest; break; }
-            }
-            now = next;
-            base += 256;
-          }
+        const int total = units * NACC;
+        const auto part_of = [&](int u) {
+          Part w;
+          w.q = NACC == 2 ? u & 1 : 0;
+          w.unit = NACC == 2 ? u >> 1 : u;
+          const int32_t *at = bounds[NACC == 2 ? w.q : pass] + (w.unit >> a.log_parts);
+          const int32_t n = at[1] - at[0], share = ((n >> a.log_parts) + 4) & ~3, first = (w.unit & (a.parts - 1)) * (int64_t)share > n ? n : (w.unit & (a.parts - 1)) * share;
+          w.from = at[0] + first;
+          w.end = at[0] + (int32_t)min((int64_t)n, (int64_t)first + share);
+          return w;
+        };
+        const auto join = [&](const Part &w, sum_t (&sum)[V]) {
           for (int off = 16; off >= 1; off >>= 1) {
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += __shfl_xor_sync(0xffffffffu, sum[v], off);
           }
           if (lane == 0) {
-            if (a.panels > 1) reached[q][unit] = stop;
 #pragma unroll
-            for (int v = 0; v < V; ++v) sums[q][unit][v] += sum[v];
+            for (int v = 0; v < V; ++v) sums[w.q][w.unit][v] += sum[v];
           }
+#pragma unroll
+          for (int v = 0; v < V; ++v) sum[v] = (sum_t)0;
+        };
+        sum_t sum[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] = (sum_t)0;
+        for (int u = warp; u < total; u += kPanelWarps) {
+          Part w = part_of(u);
+          if (several && p > 0) w.from = reached[w.q][w.unit];
+          const int32_t stop = part_sum<T, V, several>(a.src[NACC == 2 ? w.q : pass], w, c0, c1, panel, sum);
+          if (several && lane == 0) reached[w.q][w.unit] = stop;
+          join(w, sum);
         }
       }
     }
@@ -178,16 +254,16 @@ __global__ void __launch_bounds__(kPanelThreads, 1) layer_panel_kernel(const Pan
 }
 
 template <class T, int V, int NACC> comet_status_t panel_launch(Context *ctx, PanelArgs<T> &a, int64_t nnz, cudaStream_t s) {
-  const int most = kPanelSmem / (int)(V * sizeof(T));
+  const int most = kPanelSmem / (int)(V * sizeof(T)) - 1;
   a.panels = (int32_t)ceil_div(a.cols, most);
   a.panel_rows = (int32_t)align_up((size_t)ceil_div(a.cols, a.panels), 16);
   const unsigned grid = (unsigned)(a.rows < kSmCount ? a.rows : kSmCount);
   // Parts of a row: so many that every warp of a CTA has one, but of 128 entries at least.
   const int64_t rows_each = ceil_div(a.rows, grid) * NACC, mean = nnz / ((int64_t)a.rows * a.nsrc);
   a.parts = 1;
-  while (a.parts < kPanelWarps && rows_each * a.parts < kPanelWarps && mean / (a.parts * 2) >= 128) a.parts *= 2;
-  const size_t bytes = (size_t)(a.panel_rows < a.cols ? a.panel_rows : a.cols) * V * sizeof(T);
-  auto *kernel = layer_panel_kernel<T, V, NACC>;
+  while (a.parts < kPanelWarps && rows_each * a.parts < kPanelWarps && mean / (a.parts * 2) >= 128) { a.parts *= 2; ++a.log_parts; }
+  const size_t bytes = (size_t)((a.panel_rows < a.cols ? a.panel_rows : a.cols) + 1) * V * sizeof(T);
+  auto *kernel = a.panels > 1 ? layer_panel_kernel<T, V, NACC, true> : layer_panel_kernel<T, V, NACC, false>;
   COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPanelSmem));
   kernel<<<grid, kPanelThreads, bytes, s>>>(a);
   COMET_LAUNCH_CHECK(ctx);
