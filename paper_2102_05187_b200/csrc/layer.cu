@@ -77,9 +77,70 @@ bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
   return nnz >= 100000 && nnz >= 4 * rows && R * (int64_t)layer_elem_size(dtype) >= 32;
 }
 
+// fp32 and fp64 matrices of some size: the gather kernels of comet_spmm, whose tiles cut long rows and join short ones, and the epilogue in a pass of
+// its own where there is one. (Graph of 3.2 M entries, 50 columns of fp32: 470 us by a worker per row, 423 by workers that walk several rows.) They
+// keep carries in a handle's scratch; each product gets a context with scratch of its own here, so that calls may overlap.
+bool apart_fits(int dtype, const GatherCall &c) {
+  return (dtype == COMET_F64 || dtype == COMET_F32) && c.R >= 4 && c.src[0].A.nnz >= 50000;
+}
+
+comet_status_t plain_product(Context *ctx, int dtype, const GatherSource &g, int64_t R, void *C, int64_t ldc, cudaStream_t s) {
+  const int64_t es = (int64_t)layer_elem_size(dtype), most = 512 / es;       // columns of one launch of those kernels
+  for (int64_t first = 0; first < R; first += most) {
+    Context own = *ctx;
+    own.scratch = nullptr;
+    own.scratch_bytes = 0;
+    own.has_last_stream = false;
+    own.counters_dirty = false;
+    own.launches = 0;
+    const comet_status_t st = seg_gather(&own, dtype, g.A.pos + 1, g.A.crd, g.A.val, g.A.rows, g.A.nnz, (const char *)g.B + first * es, g.ldb,
+                                         R - first < most ? R - first : most, (char *)C + first * es, ldc, nullptr, g.A.rows, g.A.cols, true, false, s);
+    if (own.scratch) ctx_free(ctx, own.scratch, s);
+    ctx->launches += own.launches;
+    if (st != COMET_OK) {
+      ctx->last_cuda_error = own.last_cuda_error;
+      return st;
+    }
+  }
+  return COMET_OK;
+}
+
+bool overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t R, int64_t es) {
+  const char *x = (const char *)a, *y = (const char *)b;
+  return a && b && x < y + ((rows - 1) * ldb + R) * es && y < x + ((rows - 1) * lda + R) * es;
+}
+
+comet_status_t product_apart(Context *ctx, int dtype, const GatherCall &c, Temps &temps) {
+  const int64_t rows = c.src[0].A.rows, es = (int64_t)layer_elem_size(dtype);
+  const int n = c.mode == kLayer ? 1 : 2;
+  const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
+  if (plain) return plain_product(ctx, dtype, c.src[0], c.R, c.C, c.ldc, temps.s);
+  FinishCall f{};
+  f.rows = rows; f.R = c.R;
+  f.act = c.act; f.bias_along = c.bias_along; f.sources = n; f.sum = c.mode == kSumOfTwo;
+  f.ldz = c.ldz;
+  f.residual = c.residual; f.ldr = c.ldr;
+  f.C = c.C; f.ldc = c.ldc;
+  // Each product goes where its pre-activation is kept, or the first to C, or to temporary memory.
+  const bool kept = c.src[0].pre != nullptr;
+  const bool in_place = !kept && n == 1 && !overlap(c.residual, c.ldr, c.C, c.ldc, rows, c.R, es);
+  f.ldzin = kept ? c.ldz : in_place ? c.ldc : layer_padded(dtype, c.R);
+  for (int q = 0; q < n; ++q) {
+    void *z = kept ? c.src[q].pre : in_place ? c.C : temps.get((size_t)rows * (size_t)f.ldzin * (size_t)es);
+    if (!z) return COMET_ERR_ALLOC;
+    const comet_status_t st = plain_product(ctx, dtype, c.src[q], c.R, z, f.ldzin, temps.s);
+    if (st != COMET_OK) return st;
+    f.z[q] = z;
+    f.bias[q] = c.src[q].bias;
+    f.pre[q] = c.src[q].pre;
+  }
+  return layer_finish(ctx, dtype, f, temps.s);
+}
+
 comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
   if (c.src[0].A.rows == 0) return COMET_OK;
   if (panel_fits(dtype, c)) return layer_panel(ctx, dtype, c, temps.s);
+  if (apart_fits(dtype, c)) return product_apart(ctx, dtype, c, temps);
   const bool tiles = tile_product_fits(dtype, c);
   const int n = c.mode == kLayer ? 1 : 2;
   for (int q = 0; q < n; ++q) {

@@ -43,6 +43,20 @@ template <class T> struct Piece {
   __device__ __forceinline__ Piece() {}
 };
 
+// N neighbouring values read or written at once (2 to 16 bytes, aligned to their size).
+template <int Bytes> struct Word;
+template <> struct Word<2> { using type = unsigned short; };
+template <> struct Word<4> { using type = unsigned int; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
+template <class T, int N> struct Values {
+  using word = typename Word<(int)sizeof(T) * N>::type;
+  union { word raw; T at[N]; };
+  __device__ __forceinline__ Values() {}
+  __device__ __forceinline__ void read(const T *p) { raw = __ldcs(reinterpret_cast<const word *>(p)); }
+  __device__ __forceinline__ void write(T *p) const { *reinterpret_cast<word *>(p) = raw; }
+};
+
 // ---- activations and their slopes, in the wide type (fp32 or fp64). Fast: for results that are rounded to 16 bits, exp and the quotient from the
 // special function unit (relative errors of 2^-21 or so).
 template <bool Fast> __device__ __forceinline__ float f_exp(float x) { return Fast ? __expf(x) : expf(x); }
@@ -145,6 +159,24 @@ struct SlopeCall {
   int64_t lddz;
 };
 comet_status_t layer_slope(Context *ctx, int dtype, const SlopeCall &call, cudaStream_t s);
+
+// The epilogue on products that are there already (rows x R each): one source z0 gives f(z0 + bias0) + residual, two give f(z0 + bias0) * (z1 + bias1),
+// or, `sum`, z0 + z1. The pre-activations may be kept where they are read.
+struct FinishCall {
+  int64_t rows, R;
+  int act, bias_along, sources;
+  bool sum;
+  const void *z[2];
+  int64_t ldzin;
+  const void *bias[2];
+  void *pre[2];
+  int64_t ldz;
+  const void *residual;
+  int64_t ldr;
+  void *C;
+  int64_t ldc;
+};
+comet_status_t layer_finish(Context *ctx, int dtype, const FinishCall &call, cudaStream_t s);
 
 // A copy of a rows x R matrix with rows layer_padded values apart (the padding is not written): a whole number of 16 bytes, of 128 where the
 // tensor-core forms take 16-bit rows of 64 values and more (a tile's row is then one line).

@@ -93,6 +93,61 @@ __global__ void __launch_bounds__(kSampleThreads) layer_sample_kernel(const Samp
       row = row_of(a.pos, row0, a.rows, (int32_t)min(mine, end - 1));
     }
     row0 = __shfl_sync(0xffffffffu, row, 31);
+    if constexpr (kDeep == 8) {
+      // W is 8, 16 or 32: eight entries of a group at a time; their sums change hands while they are joined, so that W lanes end up with one entry
+      // each per W / 8 of them (7 + log2(W / 8) exchanges for eight sums instead of 8 log2(W)).
+      for (int k = 0; k < W; k += 8) {
+        if (base + (int64_t)k * G >= end) break;
+        acc_t dot[8];
+        const T *p[8], *q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int from = (k + u) * G + group;
+          p[u] = a.P + (int64_t)__shfl_sync(0xffffffffu, row, from) * a.ldp;
+          q[u] = a.Q + (int64_t)__shfl_sync(0xffffffffu, c, from) * a.ldq;
+          dot[u] = (acc_t)0;
+        }
+        sum_t wide[8];
+        int rounds = 0;
+        for (int64_t col = col0; col - col0 < a.R; col += stride, ++rounds) {  // the same number of rounds for every lane
+          T y[8][V];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) load_piece<T, V, VEC>(q[u], col, a.R, apart, y[u]);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            T x[V];
+            load_piece<T, V, VEC>(p[u], col, a.R, apart, x);
+#pragma unroll
+            for (int v = 0; v < V; ++v) dot[u] += widen(x[v]) * widen(y[u][v]);
+          }
+          if ((rounds & 15) == 15) {                                           // at most 16 V terms in the narrower type
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              wide[u] = rounds == 15 ? (sum_t)dot[u] : wide[u] + (sum_t)dot[u];
+              dot[u] = (acc_t)0;
+            }
+          }
+        }
+        if (rounds >= 16) {
+#pragma unroll
+          for (int u = 0; u < 8; ++u) dot[u] = (acc_t)(wide[u] + (sum_t)dot[u]);
+        }
+#pragma unroll
+        for (int half = 4; half >= 1; half >>= 1) {
+          const int off = W * half / 8;                                        // W / 2, W / 4, W / 8
+          const bool upper = (l & off) != 0;
+#pragma unroll
+          for (int u = 0; u < half; ++u) {
+            const acc_t give = upper ? dot[u] : dot[u + half], keep = upper ? dot[u + half] : dot[u];
+            dot[u] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+          }
+        }
+        for (int off = W / 16; off >= 1; off >>= 1) dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], off);
+        const int64_t at_entry = base + (k + l / (W / 8)) * G + group;         // the lane's bits from the top chose the halves
+        if (l % (W / 8) == 0 && at_entry < end) a.out[at_entry] = narrow<T, acc_t>(dot[0]);
+      }
+      continue;
+    }
     sum_t result = (sum_t)0;                                                 // of this lane's entry
     for (int k = 0; k < W; k += kDeep) {                                     // entries k*G .. (k+kDeep)*G of the chunk, G side by side
       sum_t dot[kDeep];
@@ -105,7 +160,7 @@ __global__ void __launch_bounds__(kSampleThreads) layer_sample_kernel(const Samp
         p[u] = a.P + (int64_t)__shfl_sync(0xffffffffu, row, from) * a.ldp;
         q[u] = a.Q + (int64_t)__shfl_sync(0xffffffffu, c, from) * a.ldq;
       }
-      for (int64_t col = col0; col - col0 < a.R; col += stride) {            // the same number of rounds for every lane
+      for (int64_t col = col0; col - col0 < a.R; col += stride) {
         T x[kDeep][V], y[kDeep][V];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) load_piece<T, V, VEC>(q[u], col, a.R, apart, y[u]);
@@ -139,7 +194,8 @@ template <class T, int V, bool VEC> comet_status_t sample_launch(Context *ctx, S
   int64_t run = align_up((size_t)ceil_div(a.nnz, (int64_t)kSmCount * 16), 32);
   a.run = (int32_t)(run > 256 ? 256 : run);
   const int64_t blocks = ceil_div(ceil_div(a.nnz, a.run), kSampleThreads / 32);
-  if (a.log_w >= 2) layer_sample_kernel<T, V, VEC, 4><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
+  if (a.log_w >= 3) layer_sample_kernel<T, V, VEC, 8><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
+  else if (a.log_w >= 2) layer_sample_kernel<T, V, VEC, 4><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   else layer_sample_kernel<T, V, VEC, 1><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   COMET_LAUNCH_CHECK(ctx);
   return COMET_OK;

@@ -3,8 +3,8 @@
 //   one source:   dz0 = dC * f'(z0)                          two (gated):  dz0 = dC * z1 * f'(z0),  dz1 = dC * f(z0)
 //   bias along the rows: sum of dz over r;  along the columns: sum of dz over i
 //
-// One pass over dC and the kept pre-activations writes dz and the sums: bound by memory. A warp per row, 32 (or, with 16-byte pieces,
-// 32 * 16 / size) columns a round, joins the row's sum by shuffles; a column's sum is taken over blocks of rows first and the blocks are added by a
+// One pass over dC and the kept pre-activations writes dz and the sums: bound by memory. As many lanes to a row as it needs, up to
+// 32, with the widest pieces that all operands' rows are aligned to, join the row's sum by shuffles; a column's sum is taken over blocks of rows first and the blocks are added by a
 // second launch in their order. Sums are held in fp32 within a lane (at most 64 terms) and in double beyond, and are taken of the
 // slopes before dz is rounded to its type.
 #include "kernels.cuh"
@@ -23,6 +23,8 @@ template <class T> struct SlopeArgs {
   int act, sources;
 };
 
+__device__ __forceinline__ int64_t ceil_to(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
 template <class T> __device__ __forceinline__ void slopes(const SlopeArgs<T> &a, typename Num<T>::acc g, typename Num<T>::acc z0, typename Num<T>::acc z1,
                                                           typename Num<T>::acc (&d)[2]) {
   if (a.sources == 1) {
@@ -33,19 +35,20 @@ template <class T> __device__ __forceinline__ void slopes(const SlopeArgs<T> &a,
   }
 }
 
-template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer_slope_kernel(const SlopeArgs<T> a) {
+// `lanes` (a power of two) to a row, V values a lane and round.
+template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer_slope_kernel(const SlopeArgs<T> a, int lanes) {
   using acc_t = typename Num<T>::acc;
-  const int lane = threadIdx.x & 31;
-  const int64_t step = (int64_t)gridDim.x * (kSlopeThreads / 32);
-  for (int64_t i = (int64_t)blockIdx.x * (kSlopeThreads / 32) + (threadIdx.x >> 5); i < a.rows; i += step) {
+  const int l = threadIdx.x & (lanes - 1), each = kSlopeThreads / lanes;
+  const int64_t step = (int64_t)gridDim.x * each, last = ceil_to(a.rows, each);
+  for (int64_t i = (int64_t)blockIdx.x * each + threadIdx.x / lanes; i < last; i += step) {           // whole warps go on together
     double sum[2] = {0.0, 0.0};
-    for (int64_t col = (int64_t)lane * V; col < a.R; col += 32 * V) {
-      Piece<T> g, z[2], out[2];
-      const bool full = V > 1 && col + V <= a.R;
+    for (int64_t col = (int64_t)l * V; col < a.R && i < a.rows; col += (int64_t)lanes * V) {
+      Values<T, V> g, z[2], out[2];
+      const bool full = V == 1 || col + V <= a.R;
       if (full) {
-        g.raw = __ldcs(reinterpret_cast<const uint4 *>(a.dC + i * a.lddc + col));
-        if (a.z[0]) z[0].raw = __ldcs(reinterpret_cast<const uint4 *>(a.z[0] + i * a.ldz + col));
-        if (a.sources == 2) z[1].raw = __ldcs(reinterpret_cast<const uint4 *>(a.z[1] + i * a.ldz + col));
+        g.read(a.dC + i * a.lddc + col);
+        if (a.z[0]) z[0].read(a.z[0] + i * a.ldz + col);
+        if (a.sources == 2) z[1].read(a.z[1] + i * a.ldz + col);
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -73,7 +76,7 @@ template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer
         sum[q] += (double)part[q];
         if (!a.dz[q]) continue;
         T *to = a.dz[q] + i * a.lddz + col;
-        if (full) *reinterpret_cast<uint4 *>(to) = out[q].raw;
+        if (full) out[q].write(to);
         else {
 #pragma unroll
           for (int v = 0; v < V; ++v)
@@ -84,10 +87,89 @@ template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       if (q >= a.sources || !a.row_bias[q]) continue;
-      for (int off = 16; off >= 1; off >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], off);
-      if (lane == 0) a.row_bias[q][i] = narrow<T, acc_t>((acc_t)sum[q]);
+      for (int off = lanes / 2; off >= 1; off >>= 1) sum[q] += __shfl_xor_sync(0xffffffffu, sum[q], off);
+      if (l == 0 && i < a.rows) a.row_bias[q][i] = narrow<T, acc_t>((acc_t)sum[q]);
     }
   }
+}
+
+template <class T> struct FinishArgs {
+  const T *z[2], *bias[2], *res;
+  T *pre[2], *C;
+  int64_t rows, R, ldzin, ldz, ldr, ldc;
+  int act, bias_along, sources;
+  bool sum;
+};
+
+template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer_finish_kernel(const FinishArgs<T> a, int lanes) {
+  using acc_t = typename Num<T>::acc;
+  const int l = threadIdx.x & (lanes - 1), each = kSlopeThreads / lanes;
+  const int64_t step = (int64_t)gridDim.x * each;
+  for (int64_t i = (int64_t)blockIdx.x * each + threadIdx.x / lanes; i < a.rows; i += step) {
+    for (int64_t col = (int64_t)l * V; col < a.R; col += (int64_t)lanes * V) {
+      Values<T, V> z[2], r, keep[2], out;
+      const bool full = V == 1 || col + V <= a.R;
+      if (full) {
+        z[0].read(a.z[0] + i * a.ldzin + col);
+        if (a.sources == 2) z[1].read(a.z[1] + i * a.ldzin + col);
+        if (a.res) r.read(a.res + i * a.ldr + col);
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (col + v >= a.R) continue;
+          z[0].at[v] = a.z[0][i * a.ldzin + col + v];
+          if (a.sources == 2) z[1].at[v] = a.z[1][i * a.ldzin + col + v];
+          if (a.res) r.at[v] = a.res[i * a.ldr + col + v];
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (!full && col + v >= a.R) continue;
+        acc_t x[2] = {widen(z[0].at[v]), a.sources == 2 ? widen(z[1].at[v]) : (acc_t)0};
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (q < a.sources && a.bias[q]) x[q] += widen(a.bias[q][a.bias_along == COMET_BIAS_ROWS ? i : col + v]);
+          keep[q].at[v] = narrow<T, acc_t>(x[q]);
+        }
+        acc_t y = a.sum ? x[0] + x[1] : activate<sizeof(T) == 2>(a.act, x[0]);
+        if (a.sources == 2 && !a.sum) y *= x[1];
+        if (a.res) y += widen(r.at[v]);
+        out.at[v] = narrow<T, acc_t>(y);
+      }
+      if (full) {
+        out.write(a.C + i * a.ldc + col);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (a.pre[q]) keep[q].write(a.pre[q] + i * a.ldz + col);
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (col + v >= a.R) continue;
+          a.C[i * a.ldc + col + v] = out.at[v];
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (a.pre[q]) a.pre[q][i * a.ldz + col + v] = keep[q].at[v];
+        }
+      }
+    }
+  }
+}
+
+// Values that can be moved at once from every row of an operand: as many as its alignment and that of its rows allow, 16 bytes at most.
+template <class T> int widest(const void *p, int64_t ld) {
+  int bytes = 16;
+  if (p)
+    while (bytes > (int)sizeof(T) && (((uintptr_t)p | (uintptr_t)(ld * (int64_t)sizeof(T))) & (uintptr_t)(bytes - 1))) bytes /= 2;
+  return bytes / (int)sizeof(T);
+}
+inline int lanes_for(int64_t R, int V) {
+  int lanes = 1;
+  while (lanes < 32 && (int64_t)lanes * V < R) lanes *= 2;
+  return lanes;
+}
+template <class T> unsigned row_grid(int64_t rows, int lanes) {
+  const int64_t blocks = ceil_div(rows, kSlopeThreads / lanes);
+  return (unsigned)(blocks < 16 * kSmCount ? blocks : 16 * kSmCount);
 }
 
 // part[block of rows, r] = the block's column sums (source 0): a thread per column
@@ -99,7 +181,7 @@ template <class T> __global__ void __launch_bounds__(kSlopeThreads) column_sums_
   const int64_t from = (int64_t)blockIdx.x * rows_per_block, to = min(a.rows, from + rows_per_block);
   double sum = 0.0;
   if (col < a.R) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = from + warp; i < to; i += kSlopeThreads / 32) {
       acc_t d[2];
       slopes(a, widen(a.dC[i * a.lddc + col]), a.z[0] ? widen(a.z[0][i * a.ldz + col]) : (acc_t)0, (acc_t)0, d);
@@ -114,17 +196,20 @@ template <class T> __global__ void __launch_bounds__(kSlopeThreads) column_sums_
   }
 }
 
-template <class T> __global__ void __launch_bounds__(kSlopeThreads) column_join_kernel(const double *__restrict__ part, int64_t blocks, int64_t R, T *__restrict__ out) {
+constexpr int kJoinThreads = 1024;
+template <class T> __global__ void __launch_bounds__(kJoinThreads) column_join_kernel(const double *__restrict__ part, int64_t blocks, int64_t R, T *__restrict__ out) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  __shared__ double joined[kSlopeThreads / 32][33];
+  __shared__ double joined[kJoinThreads / 32][33];
   const int64_t col = (int64_t)blockIdx.x * 32 + lane;
   double sum = 0.0;
-  if (col < R)
-    for (int64_t b = warp; b < blocks; b += kSlopeThreads / 32) sum += part[b * R + col];
+  if (col < R) {
+#pragma unroll 8
+    for (int64_t b = warp; b < blocks; b += kJoinThreads / 32) sum += part[b * R + col];
+  }
   joined[warp][lane] = sum;
   __syncthreads();
   if (warp == 0 && col < R) {
-    for (int w = 1; w < kSlopeThreads / 32; ++w) sum += joined[w][lane];
+    for (int w = 1; w < kJoinThreads / 32; ++w) sum += joined[w][lane];
     out[col] = narrow<T, typename Num<T>::acc>((typename Num<T>::acc)sum);
   }
 }
@@ -134,26 +219,29 @@ template <class T> comet_status_t slope_typed(Context *ctx, const SlopeCall &c, 
   a.dC = (const T *)c.dC;
   a.rows = c.rows; a.R = c.R; a.lddc = c.lddc; a.ldz = c.ldz; a.lddz = c.lddz;
   a.act = c.act; a.sources = c.sources;
-  constexpr int V = 16 / sizeof(T);
-  const auto ok = [](const void *p, int64_t ld) { return !p || (((uintptr_t)p & 15) == 0 && (ld * (int64_t)sizeof(T)) % 16 == 0); };
-  bool vec = c.R >= V && ok(c.dC, c.lddc), rows_pass = false;
+  int V = widest<T>(c.dC, c.lddc);
+  bool rows_pass = false;
   for (int q = 0; q < c.sources; ++q) {
     a.z[q] = (const T *)c.z[q];
     a.dz[q] = (T *)c.dz[q];
     if (c.bias_along == COMET_BIAS_ROWS) a.row_bias[q] = (T *)c.bias[q];
-    vec = vec && ok(c.z[q], c.ldz) && ok(c.dz[q], c.lddz);
+    const int vz = widest<T>(c.z[q], c.ldz), vd = widest<T>(c.dz[q], c.lddz);
+    V = vz < V ? vz : V;
+    V = vd < V ? vd : V;
     rows_pass = rows_pass || a.dz[q] || a.row_bias[q];
   }
   if (rows_pass) {
-    const int64_t blocks = ceil_div(c.rows, kSlopeThreads / 32);
-    const unsigned grid = (unsigned)(blocks < 16 * kSmCount ? blocks : 16 * kSmCount);
-    if (vec) layer_slope_kernel<T, V><<<grid, kSlopeThreads, 0, s>>>(a);
-    else layer_slope_kernel<T, 1><<<grid, kSlopeThreads, 0, s>>>(a);
+    const int lanes = lanes_for(c.R, V);
+    const unsigned grid = row_grid<T>(c.rows, lanes);
+    if (V * sizeof(T) == 16) layer_slope_kernel<T, 16 / sizeof(T)><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+    else if (V == 4) layer_slope_kernel<T, sizeof(T) == 2 ? 4 : 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+    else if (V == 2) layer_slope_kernel<T, sizeof(T) <= 4 ? 2 : 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+    else layer_slope_kernel<T, 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
     COMET_LAUNCH_CHECK(ctx);
   }
   if (c.bias_along == COMET_BIAS_COLS && c.bias[0]) {
     int64_t blocks = ceil_div(c.rows, 64);
-    const int64_t most = 8 * kSmCount;
+    const int64_t most = 4 * kSmCount;
     if (blocks > most) blocks = most;
     const int64_t per = ceil_div(c.rows, blocks);
     blocks = ceil_div(c.rows, per);
@@ -166,13 +254,38 @@ template <class T> comet_status_t slope_typed(Context *ctx, const SlopeCall &c, 
       if (b.z[0]) b.z[0] += first;
       b.R = c.R - first < 65535 * 32 ? c.R - first : 65535 * 32;
       column_sums_kernel<T><<<dim3((unsigned)blocks, (unsigned)ceil_div(b.R, 32)), kSlopeThreads, 0, s>>>(b, per, part);
-      column_join_kernel<T><<<(unsigned)ceil_div(b.R, 32), kSlopeThreads, 0, s>>>(part, blocks, b.R, (T *)c.bias[0] + first);
+      column_join_kernel<T><<<(unsigned)ceil_div(b.R, 32), kJoinThreads, 0, s>>>(part, blocks, b.R, (T *)c.bias[0] + first);
       ctx->launches += 2;
       e = cudaGetLastError();
     }
     ctx_free(ctx, part, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
   }
+  return COMET_OK;
+}
+
+template <class T> comet_status_t finish_typed(Context *ctx, const FinishCall &c, cudaStream_t s) {
+  FinishArgs<T> a{};
+  a.rows = c.rows; a.R = c.R; a.ldzin = c.ldzin; a.ldz = c.ldz; a.ldr = c.ldr; a.ldc = c.ldc;
+  a.act = c.act; a.bias_along = c.bias_along; a.sources = c.sources; a.sum = c.sum;
+  a.res = (const T *)c.residual;
+  a.C = (T *)c.C;
+  int V = widest<T>(c.C, c.ldc);
+  const auto also = [&](const void *p, int64_t ld) { const int v = widest<T>(p, ld); V = v < V ? v : V; };
+  also(c.residual, c.ldr);
+  for (int q = 0; q < c.sources; ++q) {
+    a.z[q] = (const T *)c.z[q];
+    a.bias[q] = (const T *)c.bias[q];
+    a.pre[q] = (T *)c.pre[q];
+    also(c.z[q], c.ldzin);
+    also(c.pre[q], c.ldz);
+  }
+  const int lanes = lanes_for(c.R, V);
+  const unsigned grid = row_grid<T>(c.rows, lanes);
+  if (V * sizeof(T) == 16) layer_finish_kernel<T, 16 / sizeof(T)><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+  else if (V == 2) layer_finish_kernel<T, sizeof(T) <= 4 ? 2 : 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+  else layer_finish_kernel<T, 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+  COMET_LAUNCH_CHECK(ctx);
   return COMET_OK;
 }
 
@@ -223,6 +336,10 @@ comet_status_t layer_slope(Context *ctx, int dtype, const SlopeCall &c, cudaStre
     case COMET_BF16: return slope_typed<__nv_bfloat16>(ctx, c, s);
     default: return slope_typed<__half>(ctx, c, s);
   }
+}
+
+comet_status_t layer_finish(Context *ctx, int dtype, const FinishCall &c, cudaStream_t s) {
+  return dtype == COMET_F64 ? finish_typed<double>(ctx, c, s) : finish_typed<float>(ctx, c, s);       // fp64 and fp32 only
 }
 
 comet_status_t layer_pick(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, void *out, cudaStream_t s) {
