@@ -11,7 +11,7 @@
 namespace comet {
 namespace {
 
-constexpr int kSampleThreads = 256;
+constexpr int kSampleThreads = 256, kMany = 8;
 
 template <class T> struct SampleArgs {
   const int32_t *pos, *crd;
@@ -61,7 +61,7 @@ __device__ __forceinline__ void load_piece(const T *p, int64_t col, int64_t R, i
 }
 
 template <class T, int V, bool VEC, int kDeep>
-__global__ void __launch_bounds__(kSampleThreads) layer_sample_kernel(const SampleArgs<T> a) {
+__global__ void __launch_bounds__(kSampleThreads, 4) layer_sample_kernel(const SampleArgs<T> a) {
   using acc_t = typename Num<T>::acc;
   using sum_t = typename Num<T>::sum;
   const int W = 1 << a.log_w, G = 32 >> a.log_w;
@@ -93,36 +93,31 @@ __global__ void __launch_bounds__(kSampleThreads) layer_sample_kernel(const Samp
       row = row_of(a.pos, row0, a.rows, (int32_t)min(mine, end - 1));
     }
     row0 = __shfl_sync(0xffffffffu, row, 31);
-    if constexpr (kDeep == 8) {
-      // W is 8, 16 or 32: eight entries of a group at a time; their sums change hands while they are joined, so that W lanes end up with one entry
-      // each per W / 8 of them (7 + log2(W / 8) exchanges for eight sums instead of 8 log2(W)).
-      for (int k = 0; k < W; k += 8) {
+    if constexpr (kDeep > 1) {
+      // kDeep entries of a group at a time (W >= kDeep); their sums change hands while they are joined, so that the lanes end up with an entry for each
+      // W / kDeep of them (with 8: 7 + log2(W / 8) exchanges for eight sums instead of 8 log2(W)).
+      for (int k = 0; k < W; k += kDeep) {
         if (base + (int64_t)k * G >= end) break;
-        acc_t dot[8];
-        const T *p[8], *q[8];
+        acc_t dot[kDeep];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int from = (k + u) * G + group;
-          p[u] = a.P + (int64_t)__shfl_sync(0xffffffffu, row, from) * a.ldp;
-          q[u] = a.Q + (int64_t)__shfl_sync(0xffffffffu, c, from) * a.ldq;
-          dot[u] = (acc_t)0;
-        }
-        sum_t wide[8];
+        for (int u = 0; u < kDeep; ++u) dot[u] = (acc_t)0;
+        const int from = k * G + group;
+        sum_t wide[kDeep];
         int rounds = 0;
         for (int64_t col = col0; col - col0 < a.R; col += stride, ++rounds) {  // the same number of rounds for every lane
-          T y[8][V];
+          T y[kDeep][V];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) load_piece<T, V, VEC>(q[u], col, a.R, apart, y[u]);
+          for (int u = 0; u < kDeep; ++u) load_piece<T, V, VEC>(a.Q + (int64_t)__shfl_sync(0xffffffffu, c, from + u * G) * a.ldq, col, a.R, apart, y[u]);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
+          for (int u = 0; u < kDeep; ++u) {
             T x[V];
-            load_piece<T, V, VEC>(p[u], col, a.R, apart, x);
+            load_piece<T, V, VEC>(a.P + (int64_t)__shfl_sync(0xffffffffu, row, from + u * G) * a.ldp, col, a.R, apart, x);
 #pragma unroll
             for (int v = 0; v < V; ++v) dot[u] += widen(x[v]) * widen(y[u][v]);
           }
           if ((rounds & 15) == 15) {                                           // at most 16 V terms in the narrower type
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < kDeep; ++u) {
               wide[u] = rounds == 15 ? (sum_t)dot[u] : wide[u] + (sum_t)dot[u];
               dot[u] = (acc_t)0;
             }
@@ -130,11 +125,11 @@ __global__ void __launch_bounds__(kSampleThreads) layer_sample_kernel(const Samp
         }
         if (rounds >= 16) {
 #pragma unroll
-          for (int u = 0; u < 8; ++u) dot[u] = (acc_t)(wide[u] + (sum_t)dot[u]);
+          for (int u = 0; u < kDeep; ++u) dot[u] = (acc_t)(wide[u] + (sum_t)dot[u]);
         }
 #pragma unroll
-        for (int half = 4; half >= 1; half >>= 1) {
-          const int off = W * half / 8;                                        // W / 2, W / 4, W / 8
+        for (int half = kDeep / 2; half >= 1; half >>= 1) {
+          const int off = W * half / kDeep;                                    // W / 2, W / 4, ..
           const bool upper = (l & off) != 0;
 #pragma unroll
           for (int u = 0; u < half; ++u) {
@@ -142,46 +137,32 @@ __global__ void __launch_bounds__(kSampleThreads) layer_sample_kernel(const Samp
             dot[u] = keep + __shfl_xor_sync(0xffffffffu, give, off);
           }
         }
-        for (int off = W / 16; off >= 1; off >>= 1) dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], off);
-        const int64_t at_entry = base + (k + l / (W / 8)) * G + group;         // the lane's bits from the top chose the halves
-        if (l % (W / 8) == 0 && at_entry < end) a.out[at_entry] = narrow<T, acc_t>(dot[0]);
+        for (int off = W / (2 * kDeep); off >= 1; off >>= 1) dot[0] += __shfl_xor_sync(0xffffffffu, dot[0], off);
+        const int64_t at_entry = base + (k + l / (W / kDeep)) * G + group;         // the lane's bits from the top chose the halves
+        if (l % (W / kDeep) == 0 && at_entry < end) a.out[at_entry] = narrow<T, acc_t>(dot[0]);
       }
       continue;
     }
+    // One to four lanes to an entry.
     sum_t result = (sum_t)0;                                                 // of this lane's entry
-    for (int k = 0; k < W; k += kDeep) {                                     // entries k*G .. (k+kDeep)*G of the chunk, G side by side
-      sum_t dot[kDeep];
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) dot[u] = (sum_t)0;
-      const T *p[kDeep], *q[kDeep];
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const int from = ((k + u) * G + group) & 31;
-        p[u] = a.P + (int64_t)__shfl_sync(0xffffffffu, row, from) * a.ldp;
-        q[u] = a.Q + (int64_t)__shfl_sync(0xffffffffu, c, from) * a.ldq;
-      }
+    for (int k = 0; k < W; ++k) {
+      const int from = k * G + group;
+      const T *p = a.P + (int64_t)__shfl_sync(0xffffffffu, row, from) * a.ldp, *q = a.Q + (int64_t)__shfl_sync(0xffffffffu, c, from) * a.ldq;
+      sum_t dot = (sum_t)0;
       for (int64_t col = col0; col - col0 < a.R; col += stride) {
-        T x[kDeep][V], y[kDeep][V];
+        T x[V], y[V];
+        load_piece<T, V, VEC>(q, col, a.R, apart, y);
+        load_piece<T, V, VEC>(p, col, a.R, apart, x);
+        acc_t t = (acc_t)0;
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u) load_piece<T, V, VEC>(q[u], col, a.R, apart, y[u]);
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) load_piece<T, V, VEC>(p[u], col, a.R, apart, x[u]);
-#pragma unroll
-        for (int u = 0; u < kDeep; ++u) {
-          acc_t t = (acc_t)0;
-#pragma unroll
-          for (int v = 0; v < V; ++v) t += widen(x[u][v]) * widen(y[u][v]);
-          dot[u] += (sum_t)t;
-        }
+        for (int v = 0; v < V; ++v) t += widen(x[v]) * widen(y[v]);
+        dot += (sum_t)t;
       }
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        for (int off = 1; off < W; off <<= 1) dot[u] += __shfl_xor_sync(0xffffffffu, dot[u], off);
-        // entry (k + u) * G + g belongs to the lane of that number; its sum sits in every lane of group g
-        const int j = at - (k + u) * G;
-        const sum_t got = __shfl_sync(0xffffffffu, dot[u], (j >= 0 && j < G ? j : 0) << a.log_w);
-        if (j >= 0 && j < G) result = got;
-      }
+      for (int off = 1; off < W; off <<= 1) dot += __shfl_xor_sync(0xffffffffu, dot, off);
+      // entry k * G + g belongs to the lane of that number; its sum sits in every lane of group g
+      const int j = at - k * G;
+      const sum_t got = __shfl_sync(0xffffffffu, dot, (j >= 0 && j < G ? j : 0) << a.log_w);
+      if (j >= 0 && j < G) result = got;
     }
     if (have) a.out[mine] = narrow<T, acc_t>((acc_t)result);
   }
@@ -194,8 +175,8 @@ template <class T, int V, bool VEC> comet_status_t sample_launch(Context *ctx, S
   int64_t run = align_up((size_t)ceil_div(a.nnz, (int64_t)kSmCount * 16), 32);
   a.run = (int32_t)(run > 256 ? 256 : run);
   const int64_t blocks = ceil_div(ceil_div(a.nnz, a.run), kSampleThreads / 32);
-  if (a.log_w >= 3) layer_sample_kernel<T, V, VEC, 8><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
-  else if (a.log_w >= 2) layer_sample_kernel<T, V, VEC, 4><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
+  if (a.log_w >= 3) layer_sample_kernel<T, V, VEC, kMany><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
+  else if (a.log_w == 2) layer_sample_kernel<T, V, VEC, 4><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   else layer_sample_kernel<T, V, VEC, 1><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   COMET_LAUNCH_CHECK(ctx);
   return COMET_OK;
