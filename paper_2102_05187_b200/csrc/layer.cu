@@ -81,7 +81,8 @@ bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
 // its own where there is one. (Graph of 3.2 M entries, 50 columns of fp32: 470 us by a worker per row, 423 by workers that walk several rows.) They
 // keep carries in a handle's scratch; each product gets a context with scratch of its own here, so that calls may overlap.
 bool apart_fits(int dtype, const GatherCall &c) {
-  return (dtype == COMET_F64 || dtype == COMET_F32) && c.R >= 4 && c.src[0].A.nnz >= 50000;
+  const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
+  return (dtype == COMET_F64 || dtype == COMET_F32) && c.R >= 4 && c.src[0].A.nnz >= (plain ? 100000 : c.mode == kLayer ? 250000 : 500000);
 }
 
 comet_status_t plain_product(Context *ctx, int dtype, const GatherSource &g, int64_t R, void *C, int64_t ldc, cudaStream_t s) {
@@ -137,12 +138,27 @@ comet_status_t product_apart(Context *ctx, int dtype, const GatherCall &c, Temps
   return layer_finish(ctx, dtype, f, temps.s);
 }
 
+// The values of a transposed matrix in its own order.
+comet_status_t pick_values(Context *ctx, int dtype, GatherSource &g, Temps &temps) {
+  void *val = temps.get((size_t)g.A.nnz * layer_elem_size(dtype));
+  if (!val) return COMET_ERR_ALLOC;
+  const comet_status_t st = layer_pick(ctx, dtype, g.A.val, g.pick, g.A.nnz, val, temps.s);
+  g.A.val = val;
+  g.pick = nullptr;
+  return st;
+}
+
 comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
   if (c.src[0].A.rows == 0) return COMET_OK;
-  if (panel_fits(dtype, c)) return layer_panel(ctx, dtype, c, temps.s);
-  if (apart_fits(dtype, c)) return product_apart(ctx, dtype, c, temps);
-  const bool tiles = tile_product_fits(dtype, c);
   const int n = c.mode == kLayer ? 1 : 2;
+  const bool panel = panel_fits(dtype, c), tiles = !panel && tile_product_fits(dtype, c);
+  for (int q = 0; q < n && !tiles; ++q) {
+    if (!c.src[q].pick) continue;
+    const comet_status_t st = pick_values(ctx, dtype, c.src[q], temps);
+    if (st != COMET_OK) return st;
+  }
+  if (panel) return layer_panel(ctx, dtype, c, temps.s);
+  if (apart_fits(dtype, c)) return product_apart(ctx, dtype, c, temps);
   for (int q = 0; q < n; ++q) {
     GatherSource &g = c.src[q];
     if (layer_aligned(dtype, g.B, g.ldb)) continue;
@@ -155,7 +171,19 @@ comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
     const comet_status_t st = pad_operand(ctx, dtype, g.B, g.ldb, g.A.cols, c.R, temps);
     if (st != COMET_OK) return st;
   }
-  return tiles ? tile_product(ctx, dtype, c, temps.s) : layer_gather(ctx, dtype, c, temps.s);
+  if (!tiles) return layer_gather(ctx, dtype, c, temps.s);
+  RowView A[2];
+  const int32_t *pick[2];
+  char *mem[2];
+  TileList lists[2];
+  for (int q = 0; q < n; ++q) {
+    A[q] = c.src[q].A;
+    pick[q] = c.src[q].pick;
+    mem[q] = (char *)temps.get(tile_list_bytes(A[q]));
+    if (!mem[q]) return COMET_ERR_ALLOC;
+  }
+  const comet_status_t st = tile_lists(ctx, A, pick, n, mem, lists, temps.s);
+  return st != COMET_OK ? st : tile_product(ctx, dtype, c, lists, temps.s);
 }
 
 comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out, Temps &temps) {
@@ -208,12 +236,10 @@ comet_status_t check_transpose(const comet_sptensor_t *A, const comet_sptensor_t
 
 bool good_act(int act) { return act >= COMET_ACT_NONE && act <= COMET_ACT_SILU; }
 
-// The values of A in At's order, for the gathers of a backward pass.
-comet_status_t view_transpose(Context *ctx, int dtype, const comet_sptensor_t *A, const comet_sptensor_t *At, Temps &temps, RowView *v) {
-  void *val = temps.get((size_t)A->nnz * layer_elem_size(dtype));
-  if (!val) return COMET_ERR_ALLOC;
-  *v = RowView{At->pos[1], At->crd[1], val, row_count(At), col_count(At), At->nnz};
-  return layer_pick(ctx, dtype, A->val, (const int32_t *)At->val, A->nnz, val, temps.s);
+// The transpose as a source of a product: its entries' values are A's, by number.
+void view_transpose(const comet_sptensor_t *A, const comet_sptensor_t *At, GatherSource *g) {
+  g->A = RowView{At->pos[1], At->crd[1], A->val, row_count(At), col_count(At), At->nnz};
+  g->pick = (const int32_t *)At->val;
 }
 
 __global__ void entry_rows_kernel(const int32_t *__restrict__ pos, int32_t rows, int64_t n, int32_t *__restrict__ row, int32_t *__restrict__ number) {
@@ -390,8 +416,7 @@ extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, co
   if (!dB) return COMET_OK;
   GatherCall c{};
   c.mode = kLayer;
-  st = view_transpose(ctx, A->dtype, A, At, temps, &c.src[0].A);
-  if (st != COMET_OK) return st;
+  view_transpose(A, At, &c.src[0]);
   c.src[0].B = dz; c.src[0].ldb = lddz;
   c.R = R;
   c.C = dB; c.ldc = lddb;
@@ -452,8 +477,7 @@ extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const
   GatherCall c{};
   c.mode = kSumOfTwo;
   for (int q = 0; q < 2; ++q) {
-    st = view_transpose(ctx, G->dtype, q ? U : G, q ? Ut : Gt, temps, &c.src[q].A);
-    if (st != COMET_OK) return st;
+    view_transpose(q ? U : G, q ? Ut : Gt, &c.src[q]);
     c.src[q].B = g.dz[q]; c.src[q].ldb = g.lddz;
   }
   c.R = R;

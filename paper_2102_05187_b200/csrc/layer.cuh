@@ -36,7 +36,16 @@ template <class T, class W> __device__ __forceinline__ T narrow(W x) { return (T
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16, float>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half narrow<__half, float>(float x) { return __float2half_rn(x); }
 
-// 16 bytes of a row as wide values, and back.
+__device__ __forceinline__ uint32_t narrow2(float low, float high, __nv_bfloat16) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(low, high);
+  return *reinterpret_cast<const uint32_t *>(&x);
+}
+__device__ __forceinline__ uint32_t narrow2(float low, float high, __half) {
+  const __half2 x = __floats2half2_rn(low, high);
+  return *reinterpret_cast<const uint32_t *>(&x);
+}
+
+// 16 bytes of a row.
 template <class T> struct Piece {
   static constexpr int kValues = 16 / sizeof(T);
   union { uint4 raw; T at[kValues]; };
@@ -91,6 +100,24 @@ template <bool Fast, class W> __device__ __forceinline__ W activate(int act, W z
   }
 }
 
+// The same on N values: what is chosen by `act` is chosen once.
+template <bool Fast, int N, class W> __device__ __forceinline__ void activate_all(int act, W (&z)[N]) {
+  if (act == COMET_ACT_NONE) return;
+  if (act == COMET_ACT_RELU) {
+#pragma unroll
+    for (int v = 0; v < N; ++v) z[v] = activate<Fast>(COMET_ACT_RELU, z[v]);
+  } else if (act == COMET_ACT_GELU) {
+#pragma unroll
+    for (int v = 0; v < N; ++v) z[v] = activate<Fast>(COMET_ACT_GELU, z[v]);
+  } else if (act == COMET_ACT_GELU_TANH) {
+#pragma unroll
+    for (int v = 0; v < N; ++v) z[v] = activate<Fast>(COMET_ACT_GELU_TANH, z[v]);
+  } else {
+#pragma unroll
+    for (int v = 0; v < N; ++v) z[v] = activate<Fast>(COMET_ACT_SILU, z[v]);
+  }
+}
+
 template <bool Fast, class W> __device__ __forceinline__ W activate_slope(int act, W z) {
   W s, rest;
   switch (act) {
@@ -116,6 +143,7 @@ inline bool layer_aligned(int dtype, const void *p, int64_t ld) { return !p || (
 // One of the up to two products of a call: its matrix, its dense operand, and, for its own pre-activation, bias and place to keep it.
 struct GatherSource {
   RowView A;
+  const int32_t *pick;     // entry p's value is val[pick[p]]; NULL: val[p]. Tensor-core form only: the others get values in order
   const void *B;
   int64_t ldb;
   const void *bias;        // NULL: none
@@ -138,9 +166,14 @@ comet_status_t layer_gather(Context *ctx, int dtype, const GatherCall &call, cud
 comet_status_t layer_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R,
                             void *out, cudaStream_t s);
 
+// A matrix's entries by tiles of 128 x 64 (layer_tile_list.cu): words of tile (t, b) at words + bases[t * (blocks + 1) + b] up to the next base.
+struct TileList { const uint32_t *words; const int32_t *bases; };
+size_t tile_list_bytes(const RowView &A);
+comet_status_t tile_lists(Context *ctx, const RowView *A, const int32_t *const *pick, int sources, char *const *mem, TileList *lists, cudaStream_t s);
+
 // The same two on the tensor cores (layer_tile_product.cu, layer_tile_sample.cu), and whether a call is one for them.
 bool tile_product_fits(int dtype, const GatherCall &call);
-comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &call, cudaStream_t s);
+comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &call, const TileList *lists, cudaStream_t s);
 // (These two want dense operands that start on 16 bytes with rows that are a whole number of 16 bytes apart.)
 bool tile_sample_fits(int dtype, const RowView &A, int64_t R);
 comet_status_t tile_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out,

@@ -291,8 +291,16 @@ template <class T> comet_status_t finish_typed(Context *ctx, const FinishCall &c
 
 template <class V> __global__ void __launch_bounds__(kBlockThreads) layer_pick_kernel(const V *__restrict__ val, const int32_t *__restrict__ index, int64_t n,
                                                                                       V *__restrict__ out) {
-  const int64_t p = (int64_t)blockIdx.x * kBlockThreads + threadIdx.x;
-  if (p < n) out[p] = __ldg(val + ld_stream(index + p));
+  const int64_t first = (int64_t)blockIdx.x * (4 * kBlockThreads) + threadIdx.x;
+  int32_t at[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) at[j] = first + j * kBlockThreads < n ? ld_stream(index + first + j * kBlockThreads) : 0;
+  V x[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = __ldg(val + at[j]);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (first + j * kBlockThreads < n) out[first + j * kBlockThreads] = x[j];
 }
 
 // A warp per row and run of 1,024 values.
@@ -344,7 +352,7 @@ comet_status_t layer_finish(Context *ctx, int dtype, const FinishCall &c, cudaSt
 
 comet_status_t layer_pick(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, void *out, cudaStream_t s) {
   if (n == 0) return COMET_OK;
-  const unsigned blocks = (unsigned)ceil_div(n, kBlockThreads);
+  const unsigned blocks = (unsigned)ceil_div(n, 4 * kBlockThreads);
   switch (layer_elem_size(dtype)) {
     case 8: layer_pick_kernel<<<blocks, kBlockThreads, 0, s>>>((const unsigned long long *)val, index, n, (unsigned long long *)out); break;
     case 4: layer_pick_kernel<<<blocks, kBlockThreads, 0, s>>>((const unsigned int *)val, index, n, (unsigned int *)out); break;
