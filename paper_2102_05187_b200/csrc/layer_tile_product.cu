@@ -41,13 +41,12 @@ template <class T> __device__ __noinline__ float stored_dot(const typename TileA
   return sum;
 }
 
-// Any alignment: a lane's four columns col, col + 32, .. of a row, as far as they lie before `limit`; a warp's lanes have neighbouring ones.
-template <class T, int NACC> __device__ __forceinline__ void finish4(const TileArgs<T> &a, int64_t i, int64_t col, int64_t limit, float (&z)[NACC][4]) {
-  float res[4];
-  if (a.res) {
+template <class T> __device__ __forceinline__ void residual4(const TileArgs<T> &a, int64_t i, int64_t col, int64_t limit, T (&res)[4]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) res[j] = col + 32 * j < limit ? widen(a.res[i * a.ldr + col + 32 * j]) : 0.0f;
-  }
+  for (int j = 0; j < 4; ++j) res[j] = a.res && i < a.rows && col + 32 * j < limit ? a.res[i * a.ldr + col + 32 * j] : (T)0.0f;
+}
+// Any alignment: a lane's four columns col, col + 32, .. of a row, as far as they lie before `limit`; a warp's lanes have neighbouring ones.
+template <class T, int NACC> __device__ __forceinline__ void finish4(const TileArgs<T> &a, int64_t i, int64_t col, int64_t limit, float (&z)[NACC][4], const T (&res)[4]) {
 #pragma unroll
   for (int q = 0; q < NACC; ++q) {
 #pragma unroll
@@ -68,8 +67,32 @@ template <class T, int NACC> __device__ __forceinline__ void finish4(const TileA
     if (col + 32 * j >= limit) continue;
     float y = z[0][j];
     if (NACC == 2) y *= z[NACC - 1][j];
-    if (a.res) y += res[j];
+    if (a.res) y += widen(res[j]);
     a.C[i * a.ldc + col + 32 * j] = narrow<T, float>(y);
+  }
+}
+
+// The rows of a tile by the sixteen warps, eight each: `cols` columns from `col` on, whose sums lie at sums[(q * apart + c) * kPitch + row].
+template <class T, int NACC>
+__device__ __noinline__ void finish_rows(const TileArgs<T> &a, int64_t row0, int64_t col, int cols, const float *sums, int apart) {
+  constexpr int kEach = kTileRows / (kTileWarps - 2);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t limit = min(a.R, col + cols);
+  for (int c = lane; col + c - lane < limit; c += 128) {
+    T res[kEach][4];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) residual4<T>(a, row0 + (warp - 2) * kEach + k, col + c, limit, res[k]);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int r = (warp - 2) * kEach + k;
+      if (row0 + r >= a.rows) break;
+      float z[NACC][4];
+#pragma unroll
+      for (int q = 0; q < NACC; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[q][j] = c + 32 * j < cols ? sums[(q * apart + c + 32 * j) * kPitch + r] : 0.0f;
+      finish4<T, NACC>(a, row0 + r, col + c, limit, z, res[k]);
+    }
   }
 }
 
@@ -178,7 +201,7 @@ struct Place {
 
 template <class T, int NACC, int kWords>
 __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const __grid_constant__ CUtensorMap map0, const __grid_constant__ CUtensorMap map1,
-                                                                          const TileArgs<T> a) {
+                                                                          const __grid_constant__ TileArgs<T> a) {
   extern __shared__ char raw_smem[];
   __shared__ uint64_t bars[2 * 8 + 1];
   __shared__ uint32_t tmem_at;
@@ -315,19 +338,7 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
         }
       }
       __syncthreads();
-      if (warp >= 2 && ok) {
-        for (int r = warp - 2; r < kTileRows && row0 + r < a.rows; r += kTileWarps - 2) {
-          const int64_t limit = min(a.R, col0 + first + min(chunk, n - first));
-          for (int c = lane; col0 + first + c - lane < limit; c += 128) {
-            float z[NACC][4];
-#pragma unroll
-            for (int q = 0; q < NACC; ++q)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) z[q][j] = c + 32 * j < chunk ? sums[(q * chunk + c + 32 * j) * kPitch + r] : 0.0f;
-            finish4<T, NACC>(a, row0 + r, col0 + first + c, limit, z);
-          }
-        }
-      }
+      if (warp >= 2 && ok) finish_rows<T, NACC>(a, row0, col0 + first, min(chunk, n - first), sums, chunk);
       tc_fence_before();
       __syncthreads();
       tc_fence_after();
@@ -356,7 +367,7 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
     const int share = n / split;
-    if (warp >= 2 && ok && a.vec_out) {
+    if (warp >= 2 && ok) {
       for (int c = part * 16; c < share; c += 16 * kParts) {
         float z[NACC][16];
 #pragma unroll
@@ -370,28 +381,19 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
 #pragma unroll
             for (int v = 0; v < 16; ++v) z[q][v] += there[(q * n + rank * share + c + v) * kPitch + quarter * 32 + lane];
         }
-        finish16<T, NACC>(a, i, col0 + rank * share + c, z);
-      }
-    } else if (warp >= 2 && ok) {
-      for (int r = warp - 2; r < kTileRows && row0 + r < a.rows; r += kTileWarps - 2) {
-        const int64_t limit = min(a.R, col0 + (rank + 1) * share);
-        for (int c = rank * share + lane; col0 + c - lane < limit; c += 128) {
-          float z[NACC][4];
+        if (a.vec_out) {
+          finish16<T, NACC>(a, i, col0 + rank * share + c, z);
+        } else {                                        // back into this CTA's own columns, which nobody else reads
 #pragma unroll
           for (int q = 0; q < NACC; ++q)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) z[q][j] = 0.0f;
-          for (int k = 0; k < split; ++k) {
-            const float *there = cluster.map_shared_rank(sums, k);
-#pragma unroll
-            for (int q = 0; q < NACC; ++q)
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (c + 32 * j < n) z[q][j] += there[(q * n + c + 32 * j) * kPitch + r];
-          }
-          finish4<T, NACC>(a, row0 + r, col0 + c, limit, z);
+            for (int v = 0; v < 16; ++v) sums[(q * n + rank * share + c + v) * kPitch + quarter * 32 + lane] = z[q][v];
         }
       }
+    }
+    if (!a.vec_out) {
+      __syncthreads();
+      if (warp >= 2 && ok) finish_rows<T, NACC>(a, row0, col0 + rank * share, share, sums + rank * share * kPitch, n);
     }
     cluster.sync();                                     // nobody's shared memory goes while another reads it
   }

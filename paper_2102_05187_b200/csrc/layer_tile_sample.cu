@@ -1,15 +1,15 @@
 // The sampled product on the tensor cores: 16-bit values and matrices whose cells are stored densely enough that computing the whole block
 // P[128 rows] Q[N rows]^T and keeping the stored cells of it costs less than a dot product per cell.
 //
-// A CTA of ten warps: one thread copies tiles of P and Q (64 values of k, by tensor map, zeros outside), one issues the products, and
-// eight warps meanwhile look up where each of the 128 rows' entries enter and leave the block's columns; then they move the block from tensor memory to
-// shared memory and write the stored cells of it, a warp per row, entries in order.
+// A CTA of eighteen warps: one thread copies tiles of P and Q (64 values of k, by tensor map, zeros outside), one issues the products, and
+// eight warps meanwhile look up where each of the 128 rows' entries enter and leave the block's columns; then sixteen move the block from tensor memory to
+// shared memory and write the stored cells of it, a warp per row, entries in order, four rows at a time.
 #include "layer_tile.cuh"
 
 namespace comet {
 namespace {
 
-constexpr int kRows = 128, kK = 64, kWarps = 10;
+constexpr int kRows = 128, kK = 64, kWarps = 18;
 constexpr int kStages = 4;
 
 template <class T> struct SampleTileArgs {
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
       }
       tc_commit(done);
     }
-  } else {
+  } else if (warp < 10) {
     // where each row's entries enter the block's columns (threads 64..191) and leave them (192..319)
     const int k = (int)threadIdx.x - 64, r = k & (kRows - 1);
     const int32_t i = row0 + r;
@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
   tc_fence_after();
   float *block = reinterpret_cast<float *>(smem);      // [n][kRows + 1]: the stages are free
   if (warp >= 2 && ok) {
-    const int quarter = warp & 3, half = (warp - 2) >> 2;
-    for (int c = half * 16; c < n; c += 32) {
+    const int quarter = warp & 3, part = (warp - 2) >> 2;
+    for (int c = part * 16; c < n; c += 16 * ((kWarps - 2) / 4)) {
       float x[16];
       tmem_load16(d + ((uint32_t)(quarter * 32) << 16) + c, x);
 #pragma unroll
@@ -105,11 +105,27 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
   tc_fence_before();
   __syncthreads();
   if (warp >= 2 && ok) {
-    for (int r = warp - 2; r < kRows; r += kWarps - 2) {
-      const int32_t to = last[r];
-      for (int32_t p = first[r] + lane; p < to; p += 32) {
-        const uint32_t c = min((uint32_t)(__ldg(a.crd + p) - col0), (uint32_t)n - 1u);
-        a.out[p] = narrow<T, float>(block[c * (kRows + 1) + r]);
+    // Four rows at a time: their first 64 entries are asked for together, what a row has beyond waits for memory.
+    constexpr int kEach = kRows / (kWarps - 2);
+#pragma unroll
+    for (int k0 = 0; k0 < kEach; k0 += 4) {
+      int32_t from[4], to[4], c[4][2];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int r = (warp - 2) * kEach + k0 + k;
+        from[k] = first[r] + lane;
+        to[k] = last[r];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) c[k][w] = from[k] + 32 * w < to[k] ? __ldg(a.crd + from[k] + 32 * w) : col0;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float *line = block + (warp - 2) * kEach + k0 + k;
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          if (from[k] + 32 * w < to[k]) a.out[from[k] + 32 * w] = narrow<T, float>(line[min((uint32_t)(c[k][w] - col0), (uint32_t)n - 1u) * (kRows + 1)]);
+        for (int32_t p = from[k] + 64; p < to[k]; p += 32)
+          a.out[p] = narrow<T, float>(line[min((uint32_t)(__ldg(a.crd + p) - col0), (uint32_t)n - 1u) * (kRows + 1)]);
       }
     }
   }
