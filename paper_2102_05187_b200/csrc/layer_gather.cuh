@@ -383,6 +383,10 @@ __global__ void __launch_bounds__(kGatherThreads, sizeof(T) == 2 ? 2 : 3) layer_
   constexpr int kPer = 32 / W;                             // entries per lane of a chunk of 32
   constexpr bool kPromote = sizeof(acc_t) != sizeof(sum_t);
   __shared__ int32_t ends[kGatherThreads / W][kWalkRows + 1];
+  __shared__ GatherArgs<T> held;                           // for the function that finishes rows: through a pointer to the parameters it took 600 cycles a value
+  static_assert(sizeof(held) % 4 == 0 && sizeof(held) / 4 <= kGatherThreads, "a word per thread");
+  if (threadIdx.x < sizeof(held) / 4) reinterpret_cast<uint32_t *>(&held)[threadIdx.x] = reinterpret_cast<const uint32_t *>(&a)[threadIdx.x];
+  __syncthreads();
   const int l = threadIdx.x & (W - 1), worker = threadIdx.x / W, first = threadIdx.x & 31 & ~(W - 1);
   const int64_t block = a.col_block0 + blockIdx.y;
   const Lane<T, V, VEC> lane(block, W, l, a.R);
@@ -416,7 +420,7 @@ __global__ void __launch_bounds__(kGatherThreads, sizeof(T) == 2 ? 2 : 3) layer_
       sum_t t[8];
 #pragma unroll
       for (int v = 0; v < 8; ++v) t[v] = v < V ? sum[v < V ? v : 0] + (sum_t)acc[v < V ? v : 0] : (sum_t)0;
-      finish_walked<T, V, VEC>(&a, (int32_t)(r0 + row), block, W, l, t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7]);
+      finish_walked<T, V, VEC>(&held, (int32_t)(r0 + row), block, W, l, t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7]);
 #pragma unroll
       for (int v = 0; v < V; ++v) { acc[v] = (acc_t)0; sum[v] = (sum_t)0; }
       ++row;

@@ -74,7 +74,7 @@ template <class T, int NACC> __device__ __forceinline__ void finish4(const TileA
 
 // The rows of a tile by the sixteen warps, eight each: `cols` columns from `col` on, whose sums lie at sums[(q * apart + c) * kPitch + row].
 template <class T, int NACC>
-__device__ __noinline__ void finish_rows(const TileArgs<T> &a, int64_t row0, int64_t col, int cols, const float *sums, int apart) {
+__device__ __forceinline__ void finish_rows(const TileArgs<T> &a, int64_t row0, int64_t col, int cols, const float *sums, int apart) {
   constexpr int kEach = kTileRows / (kTileWarps - 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t limit = min(a.R, col + cols);
