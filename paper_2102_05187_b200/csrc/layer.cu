@@ -77,12 +77,13 @@ bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
   return nnz >= 100000 && nnz >= 4 * rows && R * (int64_t)layer_elem_size(dtype) >= 32;
 }
 
-// fp32 and fp64 matrices of some size: the gather kernels of comet_spmm, whose tiles cut long rows and join short ones, and the epilogue in a pass of
-// its own where there is one. (Graph of 3.2 M entries, 50 columns of fp32: 470 us by a worker per row, 423 by workers that walk several rows.) They
-// keep carries in a handle's scratch; each product gets a context with scratch of its own here, so that calls may overlap.
+// Matrices of some size that are no case for the forms above: the gather kernels of comet_spmm, whose tiles cut long rows and join short ones, and
+// the epilogue in a pass of its own where there is one; 16-bit operands as fp32 copies. (Graph of 3.2 M entries, 50 columns of fp32: 470 us by a worker per
+// row, 173 like this; of 3.7 M entries, 64 columns of bf16: 1,590 and 210.) They keep carries in a handle's scratch; each product gets a context with
+// scratch of its own here, so that calls may overlap.
 bool apart_fits(int dtype, const GatherCall &c) {
   const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
-  return (dtype == COMET_F64 || dtype == COMET_F32) && c.R >= 4 && c.src[0].A.nnz >= (plain ? 100000 : c.mode == kLayer ? 250000 : 500000);
+  return c.R >= 4 && c.src[0].A.nnz >= (plain ? 100000 : c.mode == kLayer ? 250000 : 500000);
 }
 
 comet_status_t plain_product(Context *ctx, int dtype, const GatherSource &g, int64_t R, void *C, int64_t ldc, cudaStream_t s) {
@@ -112,10 +113,12 @@ bool overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t row
 }
 
 comet_status_t product_apart(Context *ctx, int dtype, const GatherCall &c, Temps &temps) {
-  const int64_t rows = c.src[0].A.rows, es = (int64_t)layer_elem_size(dtype);
+  const bool half = dtype == COMET_BF16 || dtype == COMET_F16;
+  const int wide = half ? (int)COMET_F32 : dtype;
+  const int64_t rows = c.src[0].A.rows, es = (int64_t)layer_elem_size(wide);
   const int n = c.mode == kLayer ? 1 : 2;
   const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
-  if (plain) return plain_product(ctx, dtype, c.src[0], c.R, c.C, c.ldc, temps.s);
+  if (plain && !half) return plain_product(ctx, dtype, c.src[0], c.R, c.C, c.ldc, temps.s);
   FinishCall f{};
   f.rows = rows; f.R = c.R;
   f.act = c.act; f.bias_along = c.bias_along; f.sources = n; f.sum = c.mode == kSumOfTwo;
@@ -123,13 +126,31 @@ comet_status_t product_apart(Context *ctx, int dtype, const GatherCall &c, Temps
   f.residual = c.residual; f.ldr = c.ldr;
   f.C = c.C; f.ldc = c.ldc;
   // Each product goes where its pre-activation is kept, or the first to C, or to temporary memory.
-  const bool kept = c.src[0].pre != nullptr;
-  const bool in_place = !kept && n == 1 && !overlap(c.residual, c.ldr, c.C, c.ldc, rows, c.R, es);
-  f.ldzin = kept ? c.ldz : in_place ? c.ldc : layer_padded(dtype, c.R);
+  const bool kept = !half && c.src[0].pre;
+  const bool in_place = !half && !kept && n == 1 && !overlap(c.residual, c.ldr, c.C, c.ldc, rows, c.R, es);
+  f.ldzin = kept ? c.ldz : in_place ? c.ldc : layer_padded(wide, c.R);
+  float *B = nullptr;
   for (int q = 0; q < n; ++q) {
+    GatherSource g = c.src[q];
+    if (half) {
+      float *val = (float *)temps.get((size_t)g.A.nnz * sizeof(float));
+      if (!val) return COMET_ERR_ALLOC;
+      comet_status_t st = layer_widen_values(ctx, dtype, g.A.val, g.pick, g.A.nnz, val, temps.s);
+      g.A.val = val;
+      g.pick = nullptr;
+      const int64_t ld = layer_padded(COMET_F32, c.R);
+      if (!B || c.mode != kGated) {                           // the gated pair has one operand
+        B = (float *)temps.get((size_t)g.A.cols * (size_t)ld * sizeof(float));
+        if (!B) return COMET_ERR_ALLOC;
+        if (st == COMET_OK) st = layer_widen(ctx, dtype, g.B, g.A.cols, c.R, g.ldb, B, temps.s);
+      }
+      if (st != COMET_OK) return st;
+      g.B = B;
+      g.ldb = ld;
+    }
     void *z = kept ? c.src[q].pre : in_place ? c.C : temps.get((size_t)rows * (size_t)f.ldzin * (size_t)es);
     if (!z) return COMET_ERR_ALLOC;
-    const comet_status_t st = plain_product(ctx, dtype, c.src[q], c.R, z, f.ldzin, temps.s);
+    const comet_status_t st = plain_product(ctx, wide, g, c.R, z, f.ldzin, temps.s);
     if (st != COMET_OK) return st;
     f.z[q] = z;
     f.bias[q] = c.src[q].bias;
@@ -151,14 +172,14 @@ comet_status_t pick_values(Context *ctx, int dtype, GatherSource &g, Temps &temp
 comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
   if (c.src[0].A.rows == 0) return COMET_OK;
   const int n = c.mode == kLayer ? 1 : 2;
-  const bool panel = panel_fits(dtype, c), tiles = !panel && tile_product_fits(dtype, c);
+  const bool panel = panel_fits(dtype, c), tiles = !panel && tile_product_fits(dtype, c), apart = !panel && !tiles && apart_fits(dtype, c);
   for (int q = 0; q < n && !tiles; ++q) {
-    if (!c.src[q].pick) continue;
+    if (!c.src[q].pick || (apart && layer_elem_size(dtype) == 2)) continue;          // widened by number there
     const comet_status_t st = pick_values(ctx, dtype, c.src[q], temps);
     if (st != COMET_OK) return st;
   }
   if (panel) return layer_panel(ctx, dtype, c, temps.s);
-  if (apart_fits(dtype, c)) return product_apart(ctx, dtype, c, temps);
+  if (apart) return product_apart(ctx, dtype, c, temps);
   for (int q = 0; q < n; ++q) {
     GatherSource &g = c.src[q];
     if (layer_aligned(dtype, g.B, g.ldb)) continue;

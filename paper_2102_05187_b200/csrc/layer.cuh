@@ -193,8 +193,8 @@ struct SlopeCall {
 };
 comet_status_t layer_slope(Context *ctx, int dtype, const SlopeCall &call, cudaStream_t s);
 
-// The epilogue on products that are there already (rows x R each): one source z0 gives f(z0 + bias0) + residual, two give f(z0 + bias0) * (z1 + bias1),
-// or, `sum`, z0 + z1. The pre-activations may be kept where they are read.
+// The epilogue on products that are there already (rows x R each, fp64 for COMET_F64, else fp32): one source z0 gives f(z0 + bias0) + residual, two give f(z0 + bias0) * (z1 + bias1),
+// or, `sum`, z0 + z1. Pre-activations of fp64 and fp32 may be kept where they are read.
 struct FinishCall {
   int64_t rows, R;
   int act, bias_along, sources;
@@ -218,6 +218,10 @@ inline int64_t layer_padded(int dtype, int64_t R) {
   return (R + v - 1) / v * v;
 }
 comet_status_t layer_pad(Context *ctx, int dtype, const void *in, int64_t rows, int64_t R, int64_t ld, void *out, cudaStream_t s);
+
+// 16-bit values as fp32: a rows x R matrix with rows layer_padded(COMET_F32, R) values apart; n values, by number where index is not NULL.
+comet_status_t layer_widen(Context *ctx, int dtype, const void *in, int64_t rows, int64_t R, int64_t ld, float *out, cudaStream_t s);
+comet_status_t layer_widen_values(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, float *out, cudaStream_t s);
 
 // out[p] = val[index[p]] for the transposed matrix's entries
 comet_status_t layer_pick(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, void *out, cudaStream_t s);

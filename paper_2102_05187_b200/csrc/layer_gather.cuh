@@ -18,18 +18,15 @@ namespace comet {
 namespace {
 
 constexpr int kGatherThreads = 256;
-constexpr int32_t kHugeRow = 16384;      // entries from which a row is cut into items of kHugeItem, in the form of a worker per row
+constexpr int32_t kHugeRow = 16384;      // entries from which a row is cut into items of kHugeItem
 constexpr int32_t kHugeItem = 4096;
-constexpr int32_t kWalkLong = 512;       // the same of the walking form
-constexpr int32_t kWalkItem = 1024;
-constexpr int kWalkRows = 8;             // most rows of a walking worker
 
 template <class T> struct GatherArgs {
   struct Source { const int32_t *pos, *crd; const T *val; const T *B; int64_t ldb; const T *bias; T *pre; } src[2];
   int64_t R, col_block0, ldc, ldr, ldz;
   T *C;
   const T *res;
-  int32_t rows, long_len, huge_len, item, rows_each;
+  int32_t rows, long_len, huge_len;
   int log_w, log_ws, act, bias_along, nsrc;
   bool gated, vec_out;
 };
@@ -269,17 +266,8 @@ __global__ void __launch_bounds__(kGatherThreads) layer_gather_kernel(const Gath
   }
 }
 
-// ---- rows that are cut into items
+// ---- rows of more than kHugeRow entries
 // counts[0]: items, counts[1]: rows. A row's items are consecutive, whatever order the rows come in.
-__device__ __forceinline__ void put_off_row(int32_t row, const int32_t (&beg)[2], const int32_t (&len)[2], int32_t item, int32_t *__restrict__ counts,
-                                            HugeItem *__restrict__ items, HugeRow *__restrict__ rows) {
-  const int32_t n0 = (int32_t)(((int64_t)len[0] + item - 1) / item), n1 = (int32_t)(((int64_t)len[1] + item - 1) / item);
-  const int32_t at = atomicAdd(counts, n0 + n1);
-  rows[atomicAdd(counts + 1, 1)] = HugeRow{row, at, n0, n1};
-  for (int q = 0; q < 2; ++q)
-    for (int32_t k = 0; k < (q ? n1 : n0); ++k) items[at + (q ? n0 : 0) + k] = HugeItem{row, q, beg[q] + k * item, min(item, len[q] - k * item)};
-}
-
 template <class T>
 __global__ void __launch_bounds__(kBlockThreads) huge_rows_kernel(const GatherArgs<T> a, int32_t *__restrict__ counts, HugeItem *__restrict__ items,
                                                                   HugeRow *__restrict__ rows) {
@@ -291,7 +279,12 @@ __global__ void __launch_bounds__(kBlockThreads) huge_rows_kernel(const GatherAr
     len[q] = __ldg(a.src[q].pos + i + 1) - beg[q];
   }
   if (max(len[0], len[1]) <= a.huge_len) return;
-  put_off_row((int32_t)i, beg, len, a.item, counts, items, rows);
+  const int32_t n0 = (int32_t)(((int64_t)len[0] + kHugeItem - 1) / kHugeItem), n1 = (int32_t)(((int64_t)len[1] + kHugeItem - 1) / kHugeItem);
+  const int32_t at = atomicAdd(counts, n0 + n1);
+  rows[atomicAdd(counts + 1, 1)] = HugeRow{(int32_t)i, at, n0, n1};
+  for (int q = 0; q < 2; ++q)
+    for (int32_t k = 0; k < (q ? n1 : n0); ++k)
+      items[at + (q ? n0 : 0) + k] = HugeItem{(int32_t)i, q, beg[q] + k * kHugeItem, min(kHugeItem, len[q] - k * kHugeItem)};
 }
 
 // part[item, 0..R) = the item's sum; a CTA per item and block of columns
@@ -359,195 +352,58 @@ __global__ void __launch_bounds__(kGatherThreads) huge_finish_kernel(const Gathe
   }
 }
 
-// ---- short rows: a worker of W lanes walks the entries of up to kWalkRows neighbouring rows in one stream, eight rows of B in flight whatever rows of A
-// they belong to, and finishes a row where its last entry has been added. (With a worker per row, rows of a few entries pay for a row's
-// whole prologue and epilogue, and their gathers wait for each other: graph of 170 thousand rows, mean 19 entries, 50 columns of fp32, 470 us.) A worker
-// that has a long row among its own puts all of them off: they are cut into items for the launches behind.
-template <class T, int V, bool VEC>
-__device__ __noinline__ void finish_walked(const GatherArgs<T> *a, int32_t row, int64_t block, int W, int l, typename Num<T>::sum s0, typename Num<T>::sum s1,
-                                           typename Num<T>::sum s2, typename Num<T>::sum s3, typename Num<T>::sum s4, typename Num<T>::sum s5,
-                                           typename Num<T>::sum s6, typename Num<T>::sum s7) {
-  const Lane<T, V, VEC> lane(block, W, l, a->R);
-  const typename Num<T>::sum all[8] = {s0, s1, s2, s3, s4, s5, s6, s7};
-  typename Num<T>::sum sum[1][V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) sum[0][v] = all[v];
-  finish_row<T, V, VEC, 1>(*a, row, lane, sum);
-}
-
-template <class T, int V, bool VEC, int W>
-__global__ void __launch_bounds__(kGatherThreads, sizeof(T) == 2 ? 2 : 3) layer_walk_kernel(const __grid_constant__ GatherArgs<T> a, int32_t *__restrict__ counts,
-                                                                                            HugeItem *__restrict__ items, HugeRow *__restrict__ put_off) {
-  using acc_t = typename Num<T>::acc;
-  using sum_t = typename Num<T>::sum;
-  constexpr int kPer = 32 / W;                             // entries per lane of a chunk of 32
-  constexpr bool kPromote = sizeof(acc_t) != sizeof(sum_t);
-  __shared__ int32_t ends[kGatherThreads / W][kWalkRows + 1];
-  __shared__ GatherArgs<T> held;                           // for the function that finishes rows: through a pointer to the parameters it took 600 cycles a value
-  static_assert(sizeof(held) % 4 == 0 && sizeof(held) / 4 <= kGatherThreads, "a word per thread");
-  if (threadIdx.x < sizeof(held) / 4) reinterpret_cast<uint32_t *>(&held)[threadIdx.x] = reinterpret_cast<const uint32_t *>(&a)[threadIdx.x];
-  __syncthreads();
-  const int l = threadIdx.x & (W - 1), worker = threadIdx.x / W, first = threadIdx.x & 31 & ~(W - 1);
-  const int64_t block = a.col_block0 + blockIdx.y;
-  const Lane<T, V, VEC> lane(block, W, l, a.R);
-  const typename GatherArgs<T>::Source &src = a.src[0];
-  const int64_t r0 = ((int64_t)blockIdx.x * (kGatherThreads / W) + worker) * a.rows_each;
-  int32_t rows = (int32_t)max((int64_t)0, min((int64_t)a.rows_each, a.rows - r0));
-  if (l < rows + 1 && rows > 0) ends[worker][l] = __ldg(src.pos + r0 + l);
-  if (W == kWalkRows && l == 0 && rows == kWalkRows) ends[worker][kWalkRows] = __ldg(src.pos + r0 + kWalkRows);
-  __syncwarp();
-  const bool is_long = l < rows && ends[worker][l + 1] - ends[worker][l] > kWalkLong;
-  if ((__ballot_sync(0xffffffffu, is_long) >> first) & (W == 32 ? 0xffffffffu : (1u << W) - 1u)) {
-    if (l == 0 && blockIdx.y == 0 && a.col_block0 == 0) {
-      for (int k = 0; k < rows; ++k) {
-        const int32_t beg[2] = {ends[worker][k], 0}, len[2] = {ends[worker][k + 1] - ends[worker][k], 0};
-        put_off_row((int32_t)(r0 + k), beg, len, kWalkItem, counts, items, put_off);
-      }
-    }
-    rows = 0;
-  }
-  const int32_t beg = rows ? ends[worker][0] : 0, total = rows ? ends[worker][rows] - beg : 0;
-  const int32_t *crd = src.crd + beg;
-  const T *val = src.val + beg;
-  acc_t acc[V];
-  sum_t sum[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) { acc[v] = (acc_t)0; sum[v] = (sum_t)0; }
-  int row = 0;
-  int32_t end = rows ? ends[worker][1] - beg : -1;           // where the current row ends, from `beg`
-  const auto finish = [&](int32_t done) {                     // the current row, and empty ones behind it
-    do {
-      sum_t t[8];
-#pragma unroll
-      for (int v = 0; v < 8; ++v) t[v] = v < V ? sum[v < V ? v : 0] + (sum_t)acc[v < V ? v : 0] : (sum_t)0;
-      finish_walked<T, V, VEC>(&held, (int32_t)(r0 + row), block, W, l, t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7]);
-#pragma unroll
-      for (int v = 0; v < V; ++v) { acc[v] = (acc_t)0; sum[v] = (sum_t)0; }
-      ++row;
-      end = row < rows ? ends[worker][row + 1] - beg : -1;
-    } while (end == done);
-  };
-  if (end == 0) finish(0);
-  const int32_t most = __reduce_max_sync(0xffffffffu, total);
-  int32_t c[kPer], next_c[kPer];
-  acc_t w[kPer], next_w[kPer];
-#pragma unroll
-  for (int p = 0; p < kPer; ++p) {
-    const int32_t i = p * W + l;
-    next_c[p] = i < total ? __ldg(crd + i) : -1;
-    next_w[p] = i < total ? widen(val[i]) : (acc_t)0;
-  }
-  const T *B = src.B + lane.col;
-  const int64_t ldb = src.ldb;
-  for (int32_t t = 0; t < most; t += 32) {
-#pragma unroll
-    for (int p = 0; p < kPer; ++p) {
-      c[p] = next_c[p];
-      w[p] = next_w[p];
-      const int32_t i = t + 32 + p * W + l;
-      next_c[p] = i < total ? __ldg(crd + i) : -1;
-      next_w[p] = i < total ? widen(val[i]) : (acc_t)0;
-    }
-#pragma unroll
-    for (int p = 0; p < kPer; ++p) {
-#pragma unroll 1
-      for (int k = 0; k < W; k += 8) {
-        const int32_t at = t + p * W + k;
-        if (at >= most) break;
-        T x[8][V];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int j = __shfl_sync(0xffffffffu, c[p], first + k + u);
-          if (lane.cols > 0 && j >= 0) lane.load(B + (int64_t)j * ldb, x[u]);
-          else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) x[u][v] = (T)0.0f;
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const acc_t y = __shfl_sync(0xffffffffu, w[p], first + k + u);
-#pragma unroll
-          for (int v = 0; v < V; ++v) acc[v] += y * widen(x[u][v]);
-          if (at + u + 1 == end) finish(at + u + 1);
-          __syncwarp();
-        }
-      }
-    }
-    if (kPromote && (t & 96) == 96) {                         // every 128 entries
-#pragma unroll
-      for (int v = 0; v < V; ++v) { sum[v] += (sum_t)acc[v]; acc[v] = (acc_t)0; }
-    }
-  }
-}
-
 inline int log2_ceil(int64_t x) {
   int k = 0;
   while ((1ll << k) < x) ++k;
   return k;
 }
 
-// Temporary memory of a call whose rows may be cut into items: at most nnz / longest rows are (twice in a pair of sources), each with an item for every
-// `item` entries and one more per source; `beside`: rows that are put off along with a long one.
-template <class T> struct PutOff {
+template <class T, int V, bool VEC, bool FEW, int NACC>
+comet_status_t gather_launch(Context *ctx, GatherArgs<T> &a, int64_t nnz, bool huge, cudaStream_t s) {
+  const int64_t per_block = (int64_t)V << a.log_w, blocks = ceil_div(a.R, per_block);
+  const unsigned groups = (unsigned)ceil_div(a.rows, kGatherThreads >> a.log_ws);
   int32_t *counts = nullptr;
   HugeItem *items = nullptr;
   HugeRow *rows = nullptr;
   typename Num<T>::sum *part = nullptr;
   char *mem = nullptr;
-  bool get(Context *ctx, int64_t nnz, int64_t R, int32_t longest, int32_t item, int beside, cudaStream_t s) {
-    const int64_t max_rows = nnz / longest * beside, max_items = nnz / item + 2 * max_rows;
+  cudaError_t e = cudaSuccess;
+  if (huge) {
+    // at most nnz / kHugeRow rows, with an item for each kHugeItem entries and at most one more per source
+    const int64_t max_rows = nnz / kHugeRow, max_items = nnz / kHugeItem + 2 * max_rows;
     const size_t b_items = align_up((size_t)max_items * sizeof(HugeItem), 256), b_rows = align_up((size_t)max_rows * sizeof(HugeRow), 256);
-    mem = (char *)ctx_alloc(ctx, 256 + b_items + b_rows + (size_t)max_items * (size_t)R * sizeof(*part), s);
+    mem = (char *)ctx_alloc(ctx, 256 + b_items + b_rows + (size_t)max_items * (size_t)a.R * sizeof(*part), s);
+    if (!mem) return COMET_ERR_ALLOC;
     counts = (int32_t *)mem;
     items = (HugeItem *)(mem + 256);
     rows = (HugeRow *)(mem + 256 + b_items);
     part = (typename Num<T>::sum *)(mem + 256 + b_items + b_rows);
-    return mem != nullptr;
-  }
-};
-
-template <class T, int V, bool VEC, bool FEW, int NACC>
-comet_status_t gather_launch(Context *ctx, GatherArgs<T> &a, int64_t nnz, bool huge, bool walks, cudaStream_t s) {
-  const int64_t per_block = (int64_t)V << a.log_w, blocks = ceil_div(a.R, per_block);
-  const unsigned groups = (unsigned)ceil_div(a.rows, kGatherThreads >> a.log_ws);
-  const unsigned walkers = walks ? (unsigned)ceil_div(ceil_div(a.rows, a.rows_each), kGatherThreads >> a.log_w) : 0;
-  PutOff<T> off;
-  if (huge && !off.get(ctx, nnz, a.R, walks ? kWalkLong : kHugeRow, a.item, walks ? a.rows_each : 1, s)) return COMET_ERR_ALLOC;
-  cudaError_t e = huge ? cudaMemsetAsync(off.counts, 0, 256, s) : cudaSuccess;
-  if (huge && !walks && e == cudaSuccess) {
-    huge_rows_kernel<T><<<(unsigned)ceil_div(a.rows, kBlockThreads), kBlockThreads, 0, s>>>(a, off.counts, off.items, off.rows);
-    ctx->launches += 1;
-    e = cudaGetLastError();
+    e = cudaMemsetAsync(counts, 0, 256, s);
+    if (e == cudaSuccess) {
+      huge_rows_kernel<T><<<(unsigned)ceil_div(a.rows, kBlockThreads), kBlockThreads, 0, s>>>(a, counts, items, rows);
+      ctx->launches += 1;
+      e = cudaGetLastError();
+    }
   }
   for (int64_t b = 0; b < blocks && e == cudaSuccess; b += 65535) {
     a.col_block0 = b;
-    const dim3 ys(1, (unsigned)(blocks - b < 65535 ? blocks - b : 65535));
-    if (walks) {
-      const dim3 grid(walkers, ys.y);
-      if constexpr (!FEW && NACC == 1) {
-        if (a.log_w == 3) layer_walk_kernel<T, V, VEC, 8><<<grid, kGatherThreads, 0, s>>>(a, off.counts, off.items, off.rows);
-        else if (a.log_w == 4) layer_walk_kernel<T, V, VEC, 16><<<grid, kGatherThreads, 0, s>>>(a, off.counts, off.items, off.rows);
-        else layer_walk_kernel<T, V, VEC, 32><<<grid, kGatherThreads, 0, s>>>(a, off.counts, off.items, off.rows);
-      }
-    } else {
-      layer_gather_kernel<T, V, VEC, FEW, NACC><<<dim3(groups, ys.y), kGatherThreads, 0, s>>>(a);
-    }
+    const unsigned ys = (unsigned)(blocks - b < 65535 ? blocks - b : 65535);
+    layer_gather_kernel<T, V, VEC, FEW, NACC><<<dim3(groups, ys), kGatherThreads, 0, s>>>(a);
     ctx->launches += 1;
     e = cudaGetLastError();
     if (huge && e == cudaSuccess) {
-      huge_items_kernel<T, V, VEC, FEW><<<dim3(4 * kSmCount, ys.y), kGatherThreads, 0, s>>>(a, off.counts, off.items, off.part);
-      huge_finish_kernel<T, V, VEC, NACC><<<dim3(kSmCount, ys.y), kGatherThreads, 0, s>>>(a, off.counts, off.rows, off.part);
+      huge_items_kernel<T, V, VEC, FEW><<<dim3(4 * kSmCount, ys), kGatherThreads, 0, s>>>(a, counts, items, part);
+      huge_finish_kernel<T, V, VEC, NACC><<<dim3(kSmCount, ys), kGatherThreads, 0, s>>>(a, counts, rows, part);
       ctx->launches += 2;
       e = cudaGetLastError();
     }
   }
-  if (off.mem) ctx_free(ctx, off.mem, s);
+  if (mem) ctx_free(ctx, mem, s);
   return e == cudaSuccess ? COMET_OK : cuda_fail(ctx, e);
 }
 
 template <class T, int V, bool VEC>
-comet_status_t gather_width(Context *ctx, GatherArgs<T> &a, int64_t nnz, int64_t most, bool huge, cudaStream_t s) {
+comet_status_t gather_width(Context *ctx, GatherArgs<T> &a, int64_t nnz, bool huge, cudaStream_t s) {
   a.log_w = log2_ceil(ceil_div(a.R, V));
   if (a.log_w > 5) a.log_w = 5;
   // Groups per worker: a quarter of a row's mean entries each, so that short rows share a warp and long ones have all of it.
@@ -556,17 +412,8 @@ comet_status_t gather_width(Context *ctx, GatherArgs<T> &a, int64_t nnz, int64_t
   if (a.log_ws > 5) a.log_ws = 5;
   const bool few = a.log_w < 3;
   if (a.gated)
-    return few ? gather_launch<T, V, VEC, true, 2>(ctx, a, nnz, huge, false, s) : gather_launch<T, V, VEC, false, 2>(ctx, a, nnz, huge, false, s);
-  if (few) return gather_launch<T, V, VEC, true, 1>(ctx, a, nnz, huge, false, s);
-  if (a.nsrc == 1 && mean < 64) {
-    // About 64 entries to a walking worker; long rows' items are shared by all lanes of a CTA.
-    a.rows_each = 1;
-    while (a.rows_each < kWalkRows && a.rows_each * (mean + 1) < 64) a.rows_each *= 2;
-    a.log_ws = 5;
-    a.item = kWalkItem;
-    return gather_launch<T, V, VEC, false, 1>(ctx, a, nnz, most > kWalkLong, true, s);
-  }
-  return gather_launch<T, V, VEC, false, 1>(ctx, a, nnz, huge, false, s);
+    return few ? gather_launch<T, V, VEC, true, 2>(ctx, a, nnz, huge, s) : gather_launch<T, V, VEC, false, 2>(ctx, a, nnz, huge, s);
+  return few ? gather_launch<T, V, VEC, true, 1>(ctx, a, nnz, huge, s) : gather_launch<T, V, VEC, false, 1>(ctx, a, nnz, huge, s);
 }
 
 inline bool aligned16(const void *p, int64_t ld, size_t es) { return !p || (((uintptr_t)p & 15) == 0 && (ld * (int64_t)es) % 16 == 0); }
@@ -602,10 +449,9 @@ template <class T> comet_status_t layer_gather_typed(Context *ctx, const GatherC
   most = most < cols ? most : cols;                          // a row's columns are distinct
   const bool huge = most > kHugeRow;
   a.huge_len = huge ? kHugeRow : 2147483647;
-  a.item = kHugeItem;
   constexpr int V = 16 / sizeof(T);
-  if (vec && c.R >= V) return gather_width<T, V, true>(ctx, a, nnz, most, huge, s);
-  return c.R >= 8 ? gather_width<T, 4, false>(ctx, a, nnz, most, huge, s) : gather_width<T, 1, false>(ctx, a, nnz, most, huge, s);
+  if (vec && c.R >= V) return gather_width<T, V, true>(ctx, a, nnz, huge, s);
+  return c.R >= 8 ? gather_width<T, 4, false>(ctx, a, nnz, huge, s) : gather_width<T, 1, false>(ctx, a, nnz, huge, s);
 }
 
 }  // namespace comet

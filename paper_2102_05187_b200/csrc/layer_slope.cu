@@ -93,8 +93,11 @@ template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer
   }
 }
 
+// Z: the products' type.
 template <class T> struct FinishArgs {
-  const T *z[2], *bias[2], *res;
+  using Z = typename Num<T>::acc;
+  const Z *z[2];
+  const T *bias[2], *res;
   T *pre[2], *C;
   int64_t rows, R, ldzin, ldz, ldr, ldc;
   int act, bias_along, sources;
@@ -107,32 +110,46 @@ template <class T, int V> __global__ void __launch_bounds__(kSlopeThreads) layer
   const int64_t step = (int64_t)gridDim.x * each;
   for (int64_t i = (int64_t)blockIdx.x * each + threadIdx.x / lanes; i < a.rows; i += step) {
     for (int64_t col = (int64_t)l * V; col < a.R; col += (int64_t)lanes * V) {
-      Values<T, V> z[2], r, keep[2], out;
+      Values<T, V> r, keep[2], out;
+      acc_t x[2][V];
       const bool full = V == 1 || col + V <= a.R;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (q >= a.sources) continue;
+        constexpr int kAtOnce = V * (int)sizeof(acc_t) <= 16 ? V : 16 / (int)sizeof(acc_t);
+        if (full) {
+#pragma unroll
+          for (int v = 0; v < V; v += kAtOnce) {
+            Values<acc_t, kAtOnce> y;
+            y.read(a.z[q] + i * a.ldzin + col + v);
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) x[q][v + k] = y.at[k];
+          }
+        } else {
+#pragma unroll
+          for (int v = 0; v < V; ++v) x[q][v] = col + v < a.R ? a.z[q][i * a.ldzin + col + v] : (acc_t)0;
+        }
+      }
       if (full) {
-        z[0].read(a.z[0] + i * a.ldzin + col);
-        if (a.sources == 2) z[1].read(a.z[1] + i * a.ldzin + col);
         if (a.res) r.read(a.res + i * a.ldr + col);
       } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           if (col + v >= a.R) continue;
-          z[0].at[v] = a.z[0][i * a.ldzin + col + v];
-          if (a.sources == 2) z[1].at[v] = a.z[1][i * a.ldzin + col + v];
           if (a.res) r.at[v] = a.res[i * a.ldr + col + v];
         }
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if (!full && col + v >= a.R) continue;
-        acc_t x[2] = {widen(z[0].at[v]), a.sources == 2 ? widen(z[1].at[v]) : (acc_t)0};
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          if (q < a.sources && a.bias[q]) x[q] += widen(a.bias[q][a.bias_along == COMET_BIAS_ROWS ? i : col + v]);
-          keep[q].at[v] = narrow<T, acc_t>(x[q]);
+          if (q >= a.sources) continue;
+          if (a.bias[q]) x[q][v] += widen(a.bias[q][a.bias_along == COMET_BIAS_ROWS ? i : col + v]);
+          keep[q].at[v] = narrow<T, acc_t>(x[q][v]);
         }
-        acc_t y = a.sum ? x[0] + x[1] : activate<sizeof(T) == 2>(a.act, x[0]);
-        if (a.sources == 2 && !a.sum) y *= x[1];
+        acc_t y = a.sum ? x[0][v] + x[1][v] : activate<sizeof(T) == 2>(a.act, x[0][v]);
+        if (a.sources == 2 && !a.sum) y *= x[1][v];
         if (a.res) y += widen(r.at[v]);
         out.at[v] = narrow<T, acc_t>(y);
       }
@@ -274,15 +291,16 @@ template <class T> comet_status_t finish_typed(Context *ctx, const FinishCall &c
   const auto also = [&](const void *p, int64_t ld) { const int v = widest<T>(p, ld); V = v < V ? v : V; };
   also(c.residual, c.ldr);
   for (int q = 0; q < c.sources; ++q) {
-    a.z[q] = (const T *)c.z[q];
+    a.z[q] = (const typename FinishArgs<T>::Z *)c.z[q];
     a.bias[q] = (const T *)c.bias[q];
     a.pre[q] = (T *)c.pre[q];
-    also(c.z[q], c.ldzin);
+    if (sizeof(T) >= 4) also(c.z[q], c.ldzin);             // (16-bit outputs: the products are this library's own, padded)
     also(c.pre[q], c.ldz);
   }
   const int lanes = lanes_for(c.R, V);
   const unsigned grid = row_grid<T>(c.rows, lanes);
   if (V * sizeof(T) == 16) layer_finish_kernel<T, 16 / sizeof(T)><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
+  else if (V == 4) layer_finish_kernel<T, sizeof(T) == 2 ? 4 : 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
   else if (V == 2) layer_finish_kernel<T, sizeof(T) <= 4 ? 2 : 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
   else layer_finish_kernel<T, 1><<<grid, kSlopeThreads, 0, s>>>(a, lanes);
   COMET_LAUNCH_CHECK(ctx);
@@ -301,6 +319,32 @@ template <class V> __global__ void __launch_bounds__(kBlockThreads) layer_pick_k
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if (first + j * kBlockThreads < n) out[first + j * kBlockThreads] = x[j];
+}
+
+template <class T> __global__ void __launch_bounds__(kBlockThreads) layer_widen_values_kernel(const T *__restrict__ val, const int32_t *__restrict__ index, int64_t n,
+                                                                                              float *__restrict__ out) {
+  const int64_t first = (int64_t)blockIdx.x * (4 * kBlockThreads) + threadIdx.x;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t p = first + j * kBlockThreads;
+    if (p < n) out[p] = widen(val[index ? (int64_t)__ldg(index + p) : p]);
+  }
+}
+
+// `lanes` to a row, four values each.
+template <class T> __global__ void __launch_bounds__(kSlopeThreads) layer_widen_kernel(const T *__restrict__ in, int64_t rows, int64_t R, int64_t ld, int64_t ldo,
+                                                                                       int lanes, float *__restrict__ out) {
+  const int l = threadIdx.x & (lanes - 1), each = kSlopeThreads / lanes;
+  for (int64_t i = (int64_t)blockIdx.x * each + threadIdx.x / lanes; i < rows; i += (int64_t)gridDim.x * each)
+    for (int64_t col = 4 * l; col < R; col += 4 * lanes) {
+      float4 x;
+      const T *p = in + i * ld + col;
+      x.x = widen(p[0]);
+      x.y = col + 1 < R ? widen(p[1]) : 0.0f;
+      x.z = col + 2 < R ? widen(p[2]) : 0.0f;
+      x.w = col + 3 < R ? widen(p[3]) : 0.0f;
+      *reinterpret_cast<float4 *>(out + i * ldo + col) = x;
+    }
 }
 
 // A warp per row and run of 1,024 values.
@@ -347,7 +391,32 @@ comet_status_t layer_slope(Context *ctx, int dtype, const SlopeCall &c, cudaStre
 }
 
 comet_status_t layer_finish(Context *ctx, int dtype, const FinishCall &c, cudaStream_t s) {
-  return dtype == COMET_F64 ? finish_typed<double>(ctx, c, s) : finish_typed<float>(ctx, c, s);       // fp64 and fp32 only
+  switch (dtype) {
+    case COMET_F64: return finish_typed<double>(ctx, c, s);
+    case COMET_F32: return finish_typed<float>(ctx, c, s);
+    case COMET_BF16: return finish_typed<__nv_bfloat16>(ctx, c, s);
+    default: return finish_typed<__half>(ctx, c, s);
+  }
+}
+
+comet_status_t layer_widen(Context *ctx, int dtype, const void *in, int64_t rows, int64_t R, int64_t ld, float *out, cudaStream_t s) {
+  if (rows == 0) return COMET_OK;
+  const int64_t ldo = layer_padded(COMET_F32, R);
+  const int lanes = lanes_for(R, 4);
+  const unsigned grid = row_grid<float>(rows, lanes);
+  if (dtype == COMET_BF16) layer_widen_kernel<<<grid, kSlopeThreads, 0, s>>>((const __nv_bfloat16 *)in, rows, R, ld, ldo, lanes, out);
+  else layer_widen_kernel<<<grid, kSlopeThreads, 0, s>>>((const __half *)in, rows, R, ld, ldo, lanes, out);
+  COMET_LAUNCH_CHECK(ctx);
+  return COMET_OK;
+}
+
+comet_status_t layer_widen_values(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, float *out, cudaStream_t s) {
+  if (n == 0) return COMET_OK;
+  const unsigned blocks = (unsigned)ceil_div(n, 4 * kBlockThreads);
+  if (dtype == COMET_BF16) layer_widen_values_kernel<<<blocks, kBlockThreads, 0, s>>>((const __nv_bfloat16 *)val, index, n, out);
+  else layer_widen_values_kernel<<<blocks, kBlockThreads, 0, s>>>((const __half *)val, index, n, out);
+  COMET_LAUNCH_CHECK(ctx);
+  return COMET_OK;
 }
 
 comet_status_t layer_pick(Context *ctx, int dtype, const void *val, const int32_t *index, int64_t n, void *out, cudaStream_t s) {
