@@ -50,11 +50,13 @@ constexpr int64_t kLdLimit = 1ll << 28;
 struct Temps {
   Context *ctx;
   cudaStream_t s;
-  void *block[16];
+  static constexpr int kMost = 32;
+  void *block[kMost];
   int count = 0;
   Temps(Context *c, cudaStream_t stream) : ctx(c), s(stream) {}
   ~Temps() { for (int i = 0; i < count; ++i) ctx_free(ctx, block[i], s); }
   void *get(size_t bytes) {
+    if (count == kMost) return nullptr;
     void *p = ctx_alloc(ctx, bytes, s);
     if (p) block[count++] = p;
     return p;
@@ -77,12 +79,15 @@ bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
   return nnz >= 100000 && nnz >= 4 * rows && R * (int64_t)layer_elem_size(dtype) >= 32;
 }
 
-// Matrices of some size that are no case for the forms above: the gather kernels of comet_spmm, whose tiles cut long rows and join short ones, and
+// Matrices of short rows (of fp64: all) that are no case for the forms above: the gather kernels of comet_spmm, whose tiles cut long rows and join short ones, and
 // the epilogue in a pass of its own where there is one; 16-bit operands as fp32 copies. (Graph of 3.2 M entries, 50 columns of fp32: 470 us by a worker per
 // row, 173 like this; of 3.7 M entries, 64 columns of bf16: 1,590 and 210.) They keep carries in a handle's scratch; each product gets a context with
 // scratch of its own here, so that calls may overlap.
 bool apart_fits(int dtype, const GatherCall &c) {
   const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
+  // Rows of some length keep a worker of their own busy, and its epilogue costs nothing: 1.7 M entries in 4,096 rows, 32 columns of fp32 33 us against
+  // 44, 16 of bf16 29 against 49; but 0.8 M entries, 100 columns of fp64 197 against 79.
+  if (dtype != COMET_F64 && c.src[0].A.nnz >= 64 * c.src[0].A.rows) return false;
   return c.R >= 4 && c.src[0].A.nnz >= (plain ? 100000 : c.mode == kLayer ? 250000 : 500000);
 }
 
@@ -207,7 +212,8 @@ comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
   return st != COMET_OK ? st : tile_product(ctx, dtype, c, lists, temps.s);
 }
 
-comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out, Temps &temps) {
+// (Q is left padded where it was copied, for a second call on it.)
+comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *&Q, int64_t &ldq, int64_t R, void *out, Temps &temps) {
   const bool tiles = tile_sample_fits(dtype, A, R);
   const bool pad_p = !layer_aligned(dtype, P, ldp), pad_q = !layer_aligned(dtype, Q, ldq);
   if (tiles || gathers_pay_padding(dtype, A.nnz, A.rows + A.cols, R)) {

@@ -482,7 +482,7 @@ bool tile_product_fits(int dtype, const GatherCall &c) {
     nnz += (double)g.A.nnz;
     cells += (double)g.A.rows * (double)g.A.cols;
   }
-  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells;      // (entry numbers run past a row by some)
+  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz * (double)c.R >= 40e6;
 }
 
 comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &c, const TileList *lists, cudaStream_t s) {

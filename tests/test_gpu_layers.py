@@ -121,6 +121,51 @@ def test_few_columns(cuda_device, dtype, R, size):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("R", [4, 33, 130])
+def test_many_short_rows(cuda_device, dtype, R):
+    """Graph-like matrices: more than half a million entries in rows of about 25, some empty, a few long ones."""
+    rows, cols, dt = 24_000, 1800, TYPES[dtype]
+    rng = np.random.default_rng(R)
+    mask = random_mask(rows, cols, 0.0145, rng, empty=(0, rows - 1, *range(500, 560)))
+    mask[7], mask[9_001, :1500], mask[rows - 2] = True, True, True
+    m = Matrix(mask, dt, rng, scale=0.2)
+    for act, bias, residual, preact, pad in [("gelu", "rows", True, True, 1), ("none", "none", False, False, 0), ("relu", "cols", True, False, 8)]:
+        out, pre, p = check_epilogue(m, dt, R, act, bias, residual, preact, rng, pad)
+        untouched(out, p)
+        if pre is not None:
+            untouched(pre, p)
+    u = Matrix(random_mask(rows, cols, 0.0145, rng), dt, rng, scale=0.2)
+    check_gated(m, u, dt, R, "silu", True, rng, pad=2)
+    check_gated(u, m, dt, R, "gelu", False, rng)
+    B, _ = values((cols, R), dt, rng)
+    r = torch.randn(rows, R, device="cuda").to(dt)
+    want = comet.spmm_epilogue(m.t, B.cuda(), act=ACTS["silu"], residual=r)
+    comet.spmm_epilogue(m.t, B.cuda(), act=ACTS["silu"], residual=r, out=r)
+    assert torch.equal(r, want)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_gradients_of_many_short_columns(cuda_device, dtype, act):
+    """The same for dB, whose matrix is the transpose: short columns; and the gated pair's sum of two products."""
+    rows, cols, R, dt = 1800, 24_000, 20, TYPES[dtype]
+    rng = np.random.default_rng(5)
+    m = Matrix(random_mask(rows, cols, 0.0145, rng, empty=(3,)), dt, rng, scale=0.2)
+    check_backward(m, dt, R, act, "cols", rng, pad=4)
+    u = Matrix(random_mask(rows, cols, 0.0145, rng), dt, rng, scale=0.2)
+    (dC, dC64), (zg, zg64), (zu, zu64) = (values((rows, R), dt, rng) for _ in range(3))
+    dB = comet.spmm_gated_backward(m.t, comet.transpose_symbolic(m.t), u.t, comet.transpose_symbolic(u.t), None, dC.cuda(), (zg.cuda(), zu.cuda()), act=ACTS[act],
+                                   need_val=False)[2]
+    dg, du = dC64 * zu64 * slope64(act, zg64), dC64 * act64(act, zg64)
+    sg = stored(dt, dg, 28 * u_of(dt) * (dC64 * zu64).abs() * (1 + zg64.abs()))
+    su = stored(dt, du, 20 * u_of(dt) * dC64.abs() * zg64.abs())
+    want = m.dense.t() @ dg + u.dense.t() @ du
+    N = m.dense.abs().t() @ (dg.abs() + sg) + u.dense.abs().t() @ (du.abs() + su)
+    bound = m.dense.abs().t() @ sg + u.dense.abs().t() @ su + 2 * z_bound(dt, m.tallest + u.tallest, N, want)     # each product may be rounded before they are added
+    assert_within(dB, want, stored(dt, want, bound), "dB")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("act", list(ACTS))
 @pytest.mark.parametrize("bias", ["none", "rows", "cols"])
 def test_epilogue_variants(cuda_device, dtype, act, bias):
@@ -449,17 +494,20 @@ def test_values_may_change_after_the_transpose(cuda_device):
     assert torch.allclose(dB, dense.t() @ dC, rtol=1e-12, atol=1e-12)
 
 
-def test_streams_and_captured_graphs(cuda_device):
-    """Calls on side streams, and two captured graphs of one handle replayed side by side."""
+@pytest.mark.parametrize("kind", ["huge row", "tiles", "short rows", "few columns"])
+def test_streams_and_captured_graphs(cuda_device, kind):
+    """Calls on side streams, and two captured graphs of one handle replayed side by side, in every form that a call may take."""
     rng = np.random.default_rng(6)
-    m = Matrix(random_mask(400, 20_000, 0.02, rng), torch.float32, rng, scale=0.1)
-    mask = m.mask.copy()
-    mask[3, :18_000] = True                                # a row that takes temporary memory
-    m = Matrix(mask, torch.float32, rng, scale=0.1)
+    rows, cols, density, R, dt = {"huge row": (400, 20_000, 0.02, 40, torch.float32), "tiles": (1024, 2048, 0.3, 128, torch.bfloat16),
+                                  "short rows": (24_000, 1800, 0.0145, 40, torch.float32), "few columns": (3000, 900, 0.3, 1, torch.float16)}[kind]
+    mask = random_mask(rows, cols, density, rng)
+    if kind == "huge row":
+        mask[3, :18_000] = True                            # a row that takes temporary memory
+    m = Matrix(mask, dt, rng, scale=0.1)
     At = comet.transpose_symbolic(m.t)
-    B = [torch.randn(20_000, 40, device="cuda") for _ in range(2)]
-    dC = [torch.randn(400, 40, device="cuda") for _ in range(2)]
-    z = [torch.randn(400, 40, device="cuda") for _ in range(2)]
+    B = [torch.randn(cols, R, device="cuda").to(dt) for _ in range(2)]
+    dC = [torch.randn(rows, R, device="cuda").to(dt) for _ in range(2)]
+    z = [torch.randn(rows, R, device="cuda").to(dt) for _ in range(2)]
 
     def step(k):
         c = comet.spmm_epilogue(m.t, B[k], act=ACTS["gelu"])
