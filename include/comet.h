@@ -315,9 +315,10 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  * Common to all of them
  *   - Matrices are [D,CU], [CU,CU] or [CN,S]; the last two get their row boundaries from a search per row into temporary memory on
  *     every call. Values and every dense operand have one type: COMET_F64, COMET_F32, COMET_BF16 or COMET_F16.
- *   - fp64 sums are held in double. fp32 products are added in fp32 over at most 128 terms and those sums in double; the 16-bit
- *     types are added in fp32. Everything between the operands and an output (bias, activation, residual) is computed in fp64 for
- *     COMET_F64 and in fp32 otherwise, and is rounded once, when the output is stored. Results do not change from run to run.
+ *   - fp64 sums are held in double. fp32 products are added in fp32 over at most 128 terms and those sums in double (or all in double); the
+ *     16-bit types are added in fp32. Everything between the operands and an output (bias, activation, residual) is computed in fp64 for
+ *     COMET_F64 and in fp32 otherwise, and is rounded once more when the output is stored; the products of large fp32 and fp64 matrices
+ *     may be rounded to their type before it. Results do not change from run to run.
  *   - Only stored cells count: infinities and NaN in rows of B that a row of A does not store do not reach that row's result.
  *   - Dense operands are row-major with any leading dimension >= R (gathered ones below 2^28 elements), aligned to one element.
  *     16-byte aligned operands with leading dimensions that are whole multiples of 16 bytes are the fastest. Outputs must not overlap
@@ -325,9 +326,11 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  *   - Asynchronous on `stream` (comet_transpose_symbolic synchronises). The handle's cached scratch is not used: temporary memory, where
  *     a call needs any, comes from the allocator and goes back to it, in stream order, before the call returns. Calls on one
  *     handle that overlap on the GPU, on several streams or in several captured graphs, are therefore allowed here as far as the allocator
- *     is stream-ordered; the host side of a handle remains one call at a time. Without an allocator (cudaMalloc) calls that
- *     need temporary memory cannot be captured: those on [CU,CU] and [CN,S] matrices, the backward passes, and products whose
- *     matrix has more than 16,384 columns.
+ *     is stream-ordered; the host side of a handle remains one call at a time. Without an allocator (cudaMalloc) most of these calls
+ *     cannot be captured.
+ *   - Which kernels a call takes follows from types, sizes and the share of stored cells: up to 16 bytes of columns read B from shared
+ *     memory; 16-bit matrices with at least 1/64 of their cells stored run on the tensor cores (8 columns and more, enough work), where about
+ *     8 bytes of temporary memory per entry are taken; short rows go through the kernels of comet_spmm, 16-bit operands as fp32 copies.
  */
 typedef enum { COMET_ACT_NONE = 0, COMET_ACT_RELU = 1, COMET_ACT_GELU = 2 /* with erf */, COMET_ACT_GELU_TANH = 3, COMET_ACT_SILU = 4 } comet_act_t;
 typedef enum { COMET_BIAS_ROWS = 0, COMET_BIAS_COLS = 1 } comet_bias_t;
@@ -343,8 +346,7 @@ typedef struct {
 } comet_epilogue_t;
 
 /* Z = A.B + bias, C = act(Z) + residual, in one pass (comet_spmm with an epilogue). h_epilogue is HOST memory, read during the call. Rows
- * without a stored entry give act(bias) + residual. Any R >= 1; R = 1 is the form for a single vector. act is applied to the
- * unrounded Z. COMET_ERR_INVALID_ARG for a NULL B, C or h_epilogue, an unknown act or bias_along, a leading dimension below R. */
+ * without a stored entry give act(bias) + residual. Any R >= 1; R = 1 is the form for a single vector. COMET_ERR_INVALID_ARG for a NULL B, C or h_epilogue, an unknown act or bias_along, a leading dimension below R. */
 comet_status_t comet_spmm_epilogue(comet_handle_t handle, const comet_sptensor_t *A, const void *B, int64_t R, int64_t ldb,
                                    const comet_epilogue_t *h_epilogue, void *C, int64_t ldc, void *stream);
 

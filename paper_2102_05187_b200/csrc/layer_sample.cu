@@ -11,7 +11,10 @@
 namespace comet {
 namespace {
 
-constexpr int kSampleThreads = 256, kMany = 8;
+constexpr int kSampleThreads = 256;
+// Entries of a group at a time, and CTAs that an SM is to hold beside each other: as many registers as eight (fp64: four) rows of Q take.
+template <class T> constexpr int kMany = sizeof(T) == 8 ? 4 : 8;
+template <class T> constexpr int kResident = sizeof(T) == 8 ? 3 : 4;
 
 template <class T> struct SampleArgs {
   const int32_t *pos, *crd;
@@ -61,7 +64,7 @@ __device__ __forceinline__ void load_piece(const T *p, int64_t col, int64_t R, i
 }
 
 template <class T, int V, bool VEC, int kDeep>
-__global__ void __launch_bounds__(kSampleThreads, 4) layer_sample_kernel(const SampleArgs<T> a) {
+__global__ void __launch_bounds__(kSampleThreads, kResident<T>) layer_sample_kernel(const SampleArgs<T> a) {
   using acc_t = typename Num<T>::acc;
   using sum_t = typename Num<T>::sum;
   const int W = 1 << a.log_w, G = 32 >> a.log_w;
@@ -171,11 +174,11 @@ __global__ void __launch_bounds__(kSampleThreads, 4) layer_sample_kernel(const S
 template <class T, int V, bool VEC> comet_status_t sample_launch(Context *ctx, SampleArgs<T> &a, cudaStream_t s) {
   a.log_w = 0;
   while (a.log_w < 5 && ((int64_t)V << a.log_w) < a.R) ++a.log_w;
-  // runs of up to 256 entries, shorter where there would not be 16 warps for every SM
-  int64_t run = align_up((size_t)ceil_div(a.nnz, (int64_t)kSmCount * 16), 32);
+  // runs of up to 256 entries, shorter where there would not be 32 warps for every SM
+  int64_t run = align_up((size_t)ceil_div(a.nnz, (int64_t)kSmCount * 32), 32);
   a.run = (int32_t)(run > 256 ? 256 : run);
   const int64_t blocks = ceil_div(ceil_div(a.nnz, a.run), kSampleThreads / 32);
-  if (a.log_w >= 3) layer_sample_kernel<T, V, VEC, kMany><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
+  if (a.log_w >= 3) layer_sample_kernel<T, V, VEC, kMany<T>><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   else if (a.log_w == 2) layer_sample_kernel<T, V, VEC, 4><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   else layer_sample_kernel<T, V, VEC, 1><<<(unsigned)blocks, kSampleThreads, 0, s>>>(a);
   COMET_LAUNCH_CHECK(ctx);
