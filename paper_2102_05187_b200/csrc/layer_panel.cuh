@@ -254,9 +254,10 @@ __global__ void __launch_bounds__(kPanelThreads, 1) layer_panel_kernel(const Pan
 }
 
 template <class T, int V, int NACC> comet_status_t panel_launch(Context *ctx, PanelArgs<T> &a, int64_t nnz, cudaStream_t s) {
-  const int most = kPanelSmem / (int)(V * sizeof(T)) - 1;
-  a.panels = (int32_t)ceil_div(a.cols, most);
-  a.panel_rows = (int32_t)align_up((size_t)ceil_div(a.cols, a.panels), 16);
+  // Panels of one size, in steps of 16 rows (they start on 16 bytes); no more than fit beside the row of zeros, and none that is empty.
+  const int most = (kPanelSmem / (int)(V * sizeof(T)) - 1) / 16 * 16;
+  a.panel_rows = (int32_t)align_up((size_t)ceil_div(a.cols, ceil_div(a.cols, most)), 16);
+  a.panels = (int32_t)ceil_div(a.cols, a.panel_rows);
   const unsigned grid = (unsigned)(a.rows < kSmCount ? a.rows : kSmCount);
   // Parts of a row: so many that every warp of a CTA has one, but of 128 entries at least.
   const int64_t rows_each = ceil_div(a.rows, grid) * NACC, mean = nnz / ((int64_t)a.rows * a.nsrc);
