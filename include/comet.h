@@ -314,7 +314,8 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  *
  * Common to all of them
  *   - Matrices are [D,CU], [CU,CU] or [CN,S]; the last two get their row boundaries from a search per row into temporary memory on
- *     every call. Values and every dense operand have one type: COMET_F64, COMET_F32, COMET_BF16 or COMET_F16.
+ *     every call. A row's entries of a [CN,S] matrix may come in any order of their columns, and a cell may be stored more than once (its
+ *     values add up, as in comet_spmm); such matrices therefore take only the kernels that need no order, not the tensor cores. Values and every dense operand have one type: COMET_F64, COMET_F32, COMET_BF16 or COMET_F16.
  *   - fp64 sums are held in double. fp32 products are added in fp32 over at most 128 terms and those sums in double (or all in double); the
  *     16-bit types are added in fp32. Everything between the operands and an output (bias, activation, residual) is computed in fp64 for
  *     COMET_F64 and in fp32 otherwise, and is rounded once more when the output is stored; the products of large fp32 and fp64 matrices
@@ -383,7 +384,8 @@ comet_status_t comet_sddmm(comet_handle_t handle, const comet_sptensor_t *A, con
                            int64_t R, void *out_val, void *stream);
 
 /* Structure of the transpose for the backward passes: the same tensor stored column by column. At is [D,CU] with A's two modes in the other
- * order, dtype COMET_I32, and At->val holds int32 numbers: entry p of At is entry At->val[p] of A. It depends on A's structure
+ * order, dtype COMET_I32, and At->val holds int32 numbers: entry p of At is entry At->val[p] of A. A cell that a [CN,S] matrix stores twice
+ * is COMET_ERR_DUPLICATE_COORD, as in comet_pack. It depends on A's structure
  * alone, is owned by the library (comet_sptensor_free) and is accepted by the backward passes only. Synchronises `stream` as comet_pack does. */
 comet_status_t comet_transpose_symbolic(comet_handle_t handle, const comet_sptensor_t *A, void *stream, comet_sptensor_t *At);
 

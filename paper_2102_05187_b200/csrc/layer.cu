@@ -12,13 +12,16 @@ template <class T> comet_status_t layer_gather_typed(Context *ctx, const GatherC
 template <class T> comet_status_t layer_panel_typed(Context *ctx, const GatherCall &c, cudaStream_t s);    // layer_panel.cuh, likewise
 
 // A few columns of matrices whose entries are worth laying B down in every SM's shared memory: rows of B of up to 16 bytes, no more of
-// them (148 times) than the matrix has bytes, and no row more than 64 times as long as the mean.
+// them (148 times) than the matrix has bytes, and no row more than 64 times as long as the mean; ordered rows where it takes several panels.
 bool panel_fits(int dtype, const GatherCall &c) {
   const double es = (double)layer_elem_size(dtype);
   if ((double)c.R * es > 16.0) return false;
   const int n = c.mode == kLayer ? 1 : 2;
+  int row_bytes = (int)layer_elem_size(dtype);
+  while (row_bytes < c.R * (int)layer_elem_size(dtype)) row_bytes *= 2;
   double nnz = 0, cells = 0;
   for (int q = 0; q < n; ++q) {
+    if (!c.src[q].A.ordered && c.src[q].A.cols > panel_capacity(row_bytes)) return false;
     nnz += (double)c.src[q].A.nnz;
     cells += (double)c.src[q].A.rows * (double)c.src[q].A.cols;
   }
@@ -81,7 +84,8 @@ bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
 
 // Matrices of short rows (of fp64: all) that are no case for the forms above: the gather kernels of comet_spmm, whose tiles cut long rows and join short ones, and
 // the epilogue in a pass of its own where there is one; 16-bit operands as fp32 copies. (Graph of 3.2 M entries, 50 columns of fp32: 470 us by a worker per
-// row, 173 like this; of 3.7 M entries, 64 columns of bf16: 1,590 and 210.) They keep carries in a handle's scratch; each product gets a context with
+// row, 173 like this; of 3.7 M entries, 64 columns of bf16: 1,590 and 210.) Rows need not be ordered for them (long ones are cut by searches
+// over one range each, whose results ascend whatever they find). They keep carries in a handle's scratch; each product gets a context with
 // scratch of its own here, so that calls may overlap.
 bool apart_fits(int dtype, const GatherCall &c) {
   const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
@@ -242,7 +246,7 @@ int64_t col_count(const comet_sptensor_t *A) { return A->dims[A->mode_order[1]];
 
 // A by rows; [CU,CU] and [CN,S] matrices get the row boundaries that [D,CU] stores from a search per row into temporary memory.
 comet_status_t view_rows(Context *ctx, const comet_sptensor_t *A, Temps &temps, RowView *v) {
-  *v = RowView{A->pos[1], A->crd[1], A->val, row_count(A), col_count(A), A->nnz};
+  *v = RowView{A->pos[1], A->crd[1], A->val, row_count(A), col_count(A), A->nnz, A->attr[1] == COMET_CU};
   if (A->attr[0] == COMET_D) return COMET_OK;
   int32_t *pos = (int32_t *)temps.get((size_t)(v->rows + 1) * sizeof(int32_t));
   if (!pos) return COMET_ERR_ALLOC;
@@ -265,7 +269,7 @@ bool good_act(int act) { return act >= COMET_ACT_NONE && act <= COMET_ACT_SILU; 
 
 // The transpose as a source of a product: its entries' values are A's, by number.
 void view_transpose(const comet_sptensor_t *A, const comet_sptensor_t *At, GatherSource *g) {
-  g->A = RowView{At->pos[1], At->crd[1], A->val, row_count(At), col_count(At), At->nnz};
+  g->A = RowView{At->pos[1], At->crd[1], A->val, row_count(At), col_count(At), At->nnz, true};
   g->pick = (const int32_t *)At->val;
 }
 

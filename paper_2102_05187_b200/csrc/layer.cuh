@@ -15,6 +15,7 @@ struct RowView {
   const int32_t *pos, *crd;
   const void *val;
   int64_t rows, cols, nnz;
+  bool ordered;            // a row's columns ascend and are distinct (compressed levels); of a caller's [CN,S] nothing is known about them
 };
 
 // The products' arithmetic. `acc`: products and short sums; `sum`: what the short sums (at most 128 terms) are added to. fp32
@@ -150,6 +151,10 @@ struct GatherSource {
   void *pre;               // NULL: not kept
 };
 enum GatherMode { kLayer, kGated, kSumOfTwo };   // f(Z) + residual; f(Z0) * Z1; Z0 + Z1 (no bias, no activation)
+constexpr int kPanelSmem = 200 * 1024;         // most shared memory of a panel of B's rows (layer_panel.cuh)
+// Rows of so many bytes that a panel holds beside the row of zeros, in steps of 16.
+constexpr int panel_capacity(int row_bytes) { return (kPanelSmem / row_bytes - 1) / 16 * 16; }
+
 struct GatherCall {
   GatherMode mode;
   GatherSource src[2];     // kLayer uses the first only
@@ -166,7 +171,7 @@ comet_status_t layer_gather(Context *ctx, int dtype, const GatherCall &call, cud
 comet_status_t layer_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R,
                             void *out, cudaStream_t s);
 
-// A matrix's entries by tiles of 128 x 64 (layer_tile_list.cu): words of tile (t, b) at words + bases[t * (blocks + 1) + b] up to the next base.
+// A matrix's entries by tiles of 128 x 64 (layer_tile_list.cu; its rows have to be ordered): words of tile (t, b) at words + bases[t * (blocks + 1) + b] up to the next base.
 struct TileList { const uint32_t *words; const int32_t *bases; };
 size_t tile_list_bytes(const RowView &A);
 comet_status_t tile_lists(Context *ctx, const RowView *A, const int32_t *const *pick, int sources, char *const *mem, TileList *lists, cudaStream_t s);

@@ -6,7 +6,7 @@
 // row, is laid down in shared memory, as many rows at a time as fit (a panel), where 32 arbitrary rows cost the bank conflicts alone. One CTA
 // of 32 warps per SM owns a stretch of rows; `parts` warps share a row, each with a contiguous part of its entries, 8 entries a lane and
 // round (4 of fp64), the next round's in flight meanwhile. A part stops where its columns leave the panel and goes on from there with the
-// next one. The parts' sums meet in shared memory and are added in their order.
+// next one, which takes ordered rows; one panel does not. The parts' sums meet in shared memory and are added in their order.
 #pragma once
 
 #include "layer.cuh"
@@ -16,7 +16,6 @@ namespace {
 
 constexpr int kPanelThreads = 1024, kPanelWarps = kPanelThreads / 32;
 constexpr int kPanelUnits = 256;               // row parts (of one source) that a CTA works on at a time
-constexpr int kPanelSmem = 200 * 1024;
 
 template <class T> struct PanelArgs {
   struct Source { const int32_t *pos, *crd; const T *val; const T *B; int64_t ldb; const T *bias; T *pre; bool aligned; } src[2];
@@ -255,7 +254,7 @@ __global__ void __launch_bounds__(kPanelThreads, 1) layer_panel_kernel(const Pan
 
 template <class T, int V, int NACC> comet_status_t panel_launch(Context *ctx, PanelArgs<T> &a, int64_t nnz, cudaStream_t s) {
   // Panels of one size, in steps of 16 rows (they start on 16 bytes); no more than fit beside the row of zeros, and none that is empty.
-  const int most = (kPanelSmem / (int)(V * sizeof(T)) - 1) / 16 * 16;
+  const int most = panel_capacity(V * (int)sizeof(T));
   a.panel_rows = (int32_t)align_up((size_t)ceil_div(a.cols, ceil_div(a.cols, most)), 16);
   a.panels = (int32_t)ceil_div(a.cols, a.panel_rows);
   const unsigned grid = (unsigned)(a.rows < kSmCount ? a.rows : kSmCount);

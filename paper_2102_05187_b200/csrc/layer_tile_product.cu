@@ -1,7 +1,7 @@
 // The sparse x dense product with its epilogue on the tensor cores: 16-bit values, matrices that are dense enough (pruned weights), 8 or more
 // columns. The stored cells of a 128 x 64 block of A are written into a zeroed tile of shared memory and multiplied as a dense tile, so
 // that every entry is read once per block of up to 256 columns and a row of B serves 128 rows of A from shared memory, where the gathers
-// fetch it once per entry.
+// fetch it once per entry. Ordered rows only: a cell has one place in the tile.
 //
 //   D[128 x N] += A_tile[128 x 64] B_tile[64 x N]        kind::f16, fp32 accumulators in tensor memory; two of them for the gated pair
 //
@@ -479,6 +479,7 @@ bool tile_product_fits(int dtype, const GatherCall &c) {
   double nnz = 0, cells = 0;
   for (int q = 0; q < n; ++q) {
     const GatherSource &g = c.src[q];
+    if (!g.A.ordered) return false;
     nnz += (double)g.A.nnz;
     cells += (double)g.A.rows * (double)g.A.cols;
   }

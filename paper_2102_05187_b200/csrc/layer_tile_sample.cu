@@ -161,7 +161,7 @@ comet_status_t sample_tiles(Context *ctx, const RowView &A, const void *P, int64
 
 bool tile_sample_fits(int dtype, const RowView &A, int64_t R) {
   if (dtype != COMET_BF16 && dtype != COMET_F16) return false;
-  if (R < 8 || R >= (1ll << 24)) return false;
+  if (R < 8 || R >= (1ll << 24) || !A.ordered) return false;          // a row's entries of a block of columns lie together
   return (double)A.nnz * 64 >= (double)A.rows * (double)A.cols && A.cols < 65535ll * 64;
 }
 
