@@ -87,6 +87,7 @@ typedef enum {
  *   COMET_MTTKRP_HOT_ROWS=0|1   per-entry MTTKRP (CSF leaf mode, COO non-root modes): never / always keep the most popular output rows in shared memory
  *                               (default: for R >= 16 and at least 2^20 entries)
  *   COMET_HOST_CHUNK_BYTES=n    comet_spmm_from_host: bytes per row of a column chunk of B and C (default 256; 0 = one chunk)
+ *   COMET_LAYER_TILE_WORK=n     layer operators: entries x columns from which 16-bit products run on the tensor cores (default 40000000)
  *   COMET_SPMM_LONG_ROWS=0      comet_spmm without the long-row path; COMET_SPMM_LONG_ROW, _LONG_TILE, _PIECE,
  *                               _BLOCK_MB, _BLOCKS, _LONG_CTAS, _LONG_MIN_NNZ, _LONG_MIN_B_MB: its threshold
  *                               (entries), tile and piece sizes, block size / count of B, CTAs of the long-row

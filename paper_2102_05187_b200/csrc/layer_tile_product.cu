@@ -13,6 +13,8 @@
 
 #include "layer_tile.cuh"
 
+#include <stdlib.h>
+
 namespace cg = cooperative_groups;
 
 namespace comet {
@@ -472,6 +474,12 @@ template <class T> comet_status_t product_typed(Context *ctx, const GatherCall &
 
 }  // namespace
 
+// Entries x columns from which a product is one for tiles.
+static double least_work() {
+  const char *e = getenv("COMET_LAYER_TILE_WORK");
+  return e ? atof(e) : 40e6;
+}
+
 bool tile_product_fits(int dtype, const GatherCall &c) {
   if (dtype != COMET_BF16 && dtype != COMET_F16) return false;
   if (c.R < 8 || c.R >= (1ll << 24)) return false;
@@ -483,7 +491,7 @@ bool tile_product_fits(int dtype, const GatherCall &c) {
     nnz += (double)g.A.nnz;
     cells += (double)g.A.rows * (double)g.A.cols;
   }
-  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz * (double)c.R >= 40e6;
+  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz * (double)c.R >= least_work();
 }
 
 comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &c, const TileList *lists, cudaStream_t s) {

@@ -58,3 +58,24 @@ def test_full_panels_of_the_transpose(cuda_device, dtype, R, cols, rows, density
     e = N * (u_of(dt) * 4 + (torch.finfo(dt).eps / 2 if dt in (torch.bfloat16, torch.float16) else 0))
     tiny = 2.0 ** -25 * (m.dense.abs().sum(0) + u.dense.abs().sum(0))[:, None] if dt == torch.float16 else 0.0      # dZ below fp16's normal range
     assert_within(dB, want, stored(dt, want, 1.01 * e + tiny + z_bound(dt, m.tallest + u.tallest, N * 1.01, want)), "dB")
+
+
+@pytest.mark.parametrize("dtype,R,cols,rows,density", [("bf16", 8, 2000, 400, 0.5), ("f32", 1, 3000, 700, 0.4), ("f64", 2, 25_580, 500, 0.5), ("bf16", 8, 25_570, 900, 0.5)])
+def test_only_stored_cells_count_in_panels(cuda_device, dtype, R, cols, rows, density):
+    """Infinities and NaN in rows of B that a row of A does not store leave its result alone, in the panel that holds them and in the others."""
+    dt = TYPES[dtype]
+    rng = np.random.default_rng(cols)
+    mask = mask_of(rows, cols, density, rng)
+    bad = [0, 9, cols // 2 - 1, cols // 2, cols - 9, cols - 1]
+    mask[:, bad] = False
+    mask[rows - 50:, bad[2]] = True
+    m = Matrix(mask, dt, rng, scale=(cols * density) ** -0.5)
+    B, _ = values((cols, R), dt, rng)
+    for k, j in enumerate(bad):
+        B[j] = [float("nan"), float("inf"), float("nan"), -float("inf"), float("inf"), float("nan")][k]
+    B64 = torch.nan_to_num(B.double(), nan=0.0, posinf=0.0, neginf=0.0)
+    got = comet.spmm_epilogue(m.t, B.cuda()).cpu()
+    assert bool(torch.isnan(got[rows - 50:]).all())
+    z = m.dense @ B64
+    bound = stored(dt, z, z_bound(dt, m.longest, m.dense.abs() @ B64.abs(), z))
+    assert_within(got[:rows - 50], z[:rows - 50], bound[:rows - 50], "rows without them")
