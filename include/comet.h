@@ -88,6 +88,7 @@ typedef enum {
  *                               (default: for R >= 16 and at least 2^20 entries)
  *   COMET_HOST_CHUNK_BYTES=n    comet_spmm_from_host: bytes per row of a column chunk of B and C (default 256; 0 = one chunk)
  *   COMET_LAYER_TILE_WORK=n     layer operators: entries x columns from which 16-bit products run on the tensor cores (default 40000000)
+ *   COMET_LAYER_WAIT_CYCLES=n   layer operators: cycles after which a wait of the tensor-core kernels gives up (default 8000000000; 0: at once)
  *   COMET_SPMM_LONG_ROWS=0      comet_spmm without the long-row path; COMET_SPMM_LONG_ROW, _LONG_TILE, _PIECE,
  *                               _BLOCK_MB, _BLOCKS, _LONG_CTAS, _LONG_MIN_NNZ, _LONG_MIN_B_MB: its threshold
  *                               (entries), tile and piece sizes, block size / count of B, CTAs of the long-row
@@ -330,6 +331,10 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  *     handle that overlap on the GPU, on several streams or in several captured graphs, are therefore allowed here as far as the allocator
  *     is stream-ordered; the host side of a handle remains one call at a time. Without an allocator (cudaMalloc) most of these calls
  *     cannot be captured.
+ *   - The waits inside the tensor-core kernels end after about four seconds. A kernel whose wait ran out returns with its outputs in part
+ *     unwritten, after its call has returned COMET_OK; the next call of a layer operator on the handle then returns COMET_ERR_CUDA (with
+ *     cudaErrorLaunchTimeout as its comet_last_cuda_error) and launches nothing, and the one after it works again. Calls captured into a graph
+ *     report in the same way, to the next call made outside of it.
  *   - Which kernels a call takes follows from types, sizes and the share of stored cells: up to 16 bytes of columns read B from shared
  *     memory; 16-bit matrices with at least 1/64 of their cells stored run on the tensor cores (8 columns and more, enough work), where about
  *     8 bytes of temporary memory per entry are taken; short rows go through the kernels of comet_spmm, 16-bit operands as fp32 copies.

@@ -91,7 +91,7 @@ extern "C" comet_status_t comet_create(comet_handle_t *handle, const comet_alloc
     delete ctx;
     return COMET_ERR_CUDA;
   }
-  for (int i = 0; i < 64; ++i) ctx->h_pinned[i] = 0;          // word 63: see layer_tile.cuh
+  for (int i = 0; i < 64; ++i) ctx->h_pinned[i] = 0;          // word 63: see layer.cuh
   // words 32.. hold counters that kernels leave at zero when they finish (see contract_scalar.cu)
   if (cudaMemset(ctx->d_status, 0, 64 * sizeof(int32_t)) != cudaSuccess) {
     cudaGetLastError();

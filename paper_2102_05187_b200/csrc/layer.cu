@@ -3,9 +3,15 @@
 #include "kernels.cuh"
 #include "layer.cuh"
 
+#include <stdlib.h>
 #include <string.h>
 
 namespace comet {
+
+int64_t wait_patience() {
+  const char *e = getenv("COMET_LAYER_WAIT_CYCLES");
+  return e ? atoll(e) : 8000000000ll;                      // about four seconds
+}
 
 template <class T> comet_status_t layer_gather_typed(Context *ctx, const GatherCall &c, cudaStream_t s);   // layer_gather.cuh, a unit per type
 
@@ -229,6 +235,15 @@ comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P,
   return tiles ? tile_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s) : layer_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s);
 }
 
+// What a kernel of an earlier call has left behind that gave up: COMET_ERR_CUDA once, COMET_OK otherwise.
+comet_status_t earlier_calls(Context *ctx) {
+  volatile int32_t *word = ctx->h_pinned + kLayerStatusWord;
+  if (!*word) return COMET_OK;
+  *word = 0;
+  ctx->last_cuda_error = (int)cudaErrorLaunchTimeout;
+  return COMET_ERR_CUDA;
+}
+
 bool off_type(const void *p, size_t es) { return ((uintptr_t)p & (es - 1)) != 0; }
 
 comet_status_t check_matrix(const comet_sptensor_t *A) {
@@ -302,6 +317,7 @@ extern "C" comet_status_t comet_spmm_epilogue(comet_handle_t handle, const comet
   if (off_type(B, es) || off_type(C, es) || off_type(e.bias, es) || off_type(e.residual, es) || off_type(e.preact, es)) return COMET_ERR_MISALIGNED;
   if (ldb >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
   Context *ctx = reinterpret_cast<Context *>(handle);
+  if ((st = earlier_calls(ctx)) != COMET_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
   Temps temps(ctx, s);
   GatherCall c{};
@@ -332,6 +348,7 @@ extern "C" comet_status_t comet_spmm_gated(comet_handle_t handle, const comet_sp
     return COMET_ERR_MISALIGNED;
   if (ldb >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
   Context *ctx = reinterpret_cast<Context *>(handle);
+  if ((st = earlier_calls(ctx)) != COMET_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
   Temps temps(ctx, s);
   GatherCall c{};
@@ -362,6 +379,7 @@ extern "C" comet_status_t comet_sddmm(comet_handle_t handle, const comet_sptenso
   if (ldp >= kLdLimit || ldq >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
   if (A->nnz == 0) return COMET_OK;
   Context *ctx = reinterpret_cast<Context *>(handle);
+  if ((st = earlier_calls(ctx)) != COMET_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
   Temps temps(ctx, s);
   RowView v;
@@ -377,6 +395,7 @@ extern "C" comet_status_t comet_transpose_symbolic(comet_handle_t handle, const 
   comet_status_t st = check_matrix(A);
   if (st != COMET_OK) return st;
   Context *ctx = reinterpret_cast<Context *>(handle);
+  if ((st = earlier_calls(ctx)) != COMET_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
   Temps temps(ctx, s);
   int32_t *row = (int32_t *)temps.get((size_t)A->nnz * sizeof(int32_t)), *number = (int32_t *)temps.get((size_t)A->nnz * sizeof(int32_t));
@@ -414,6 +433,7 @@ extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, co
     return COMET_ERR_MISALIGNED;
   if ((dval && ldb >= kLdLimit) || lddc >= kLdLimit || R >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
   Context *ctx = reinterpret_cast<Context *>(handle);
+  if ((st = earlier_calls(ctx)) != COMET_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
   Temps temps(ctx, s);
   const void *dz = dC;
@@ -477,6 +497,7 @@ extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const
     return COMET_ERR_MISALIGNED;
   if ((dvals && ldb >= kLdLimit) || R >= kLdLimit) return COMET_ERR_INDEX_OVERFLOW;
   Context *ctx = reinterpret_cast<Context *>(handle);
+  if ((st = earlier_calls(ctx)) != COMET_OK) return st;
   cudaStream_t s = (cudaStream_t)stream;
   Temps temps(ctx, s);
   SlopeCall g{};

@@ -167,6 +167,9 @@ struct GatherCall {
 };
 comet_status_t layer_gather(Context *ctx, int dtype, const GatherCall &call, cudaStream_t s);
 
+constexpr int kLayerStatusWord = 63;           // of Context::h_pinned: set by a tensor-core kernel that gave up (layer_tile.cuh), read by the next layer call
+int64_t wait_patience();                       // cycles that a wait of those kernels may take
+
 // out[p] = sum over r of P[row of p, r] * Q[crd[p], r]
 comet_status_t layer_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R,
                             void *out, cudaStream_t s);

@@ -8,10 +8,10 @@
 
 namespace comet {
 
-// Every wait gives up after this many cycles (some seconds): the kernel then notes it, gives its copies time to land, frees its tensor memory and
-// returns. (The cycle counter, not the global timer: reading that one took longer than most waits.)
-constexpr int64_t kWaitCycles = 8000000000ll;
-constexpr int kTileStatusWord = 63;            // of Context::h_pinned: set by a kernel that gave up, read by the next call
+// Every wait gives up after some seconds (`patience`, in cycles; 0: `failed` from the start): the kernel then skips the rest, waits for its products and
+// copies in flight, frees its tensor memory, sets a word of the handle's pinned memory and returns. The next call of a layer operator reports it.
+// (The cycle counter, not the global timer: reading that one took longer than most waits.)
+constexpr int64_t kEndCycles = 4000000000ll;   // for what is in flight at the end, which nothing can hold up
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -35,20 +35,25 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return done != 0;
 }
-// False once a wait of this CTA has run out (then and from then on).
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
+// False once a wait of this CTA has run out (then and from then on, unless the barrier is there already).
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed, int64_t patience) {
   if (bar_try(bar, parity)) return true;
   const int64_t since = clock64();
   while (!*failed) {
     for (int i = 0; i < 64; ++i)
       if (bar_try(bar, parity)) return true;
-    if (clock64() - since > kWaitCycles) *failed = 1;
+    if (clock64() - since > patience) *failed = 1;
   }
   return false;
 }
 // The same for a warp whose lanes go on together.
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *failed) {
-  return __all_sync(0xffffffffu, bar_wait(bar, parity, failed));
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *failed, int64_t patience) {
+  return __all_sync(0xffffffffu, bar_wait(bar, parity, failed, patience));
+}
+// For what a CTA that gives up has in flight.
+__device__ __forceinline__ void bar_wait_end(uint32_t bar, uint32_t parity) {
+  const int64_t since = clock64();
+  while (!bar_try(bar, parity) && clock64() - since < kEndCycles) {}
 }
 
 __device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap *map, int x, int y, uint32_t bar) {
@@ -84,11 +89,11 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// At the end of a CTA whose waits have run out (one thread): copies in flight land before the shared memory is given up, and the host is told.
-__device__ __forceinline__ void give_up(uint32_t full, int stages, int32_t *status) {
-  const int64_t since = clock64();
-  for (int s = 0; s < stages; ++s)
-    while (!bar_try(full + 8 * s, 0) && clock64() - since < kWaitCycles) {}
+// At the end of a CTA whose waits have run out, by the thread that issued the copies, `issued` of them, one stage after the other: the last one of every
+// stage lands before the shared memory is given up (the ones before it have: its stage was free), and the host is told. Nothing but the
+// copies completes the barriers at `landed`.
+__device__ __forceinline__ void give_up(uint32_t landed, int stages, int32_t issued, int32_t *status) {
+  for (int s = 0; s < stages && s < issued; ++s) bar_wait_end(landed + 8 * s, (uint32_t)((issued - 1 - s) / stages) & 1);
   *(volatile int32_t *)status = 1;
   __threadfence_system();
 }
@@ -119,13 +124,5 @@ __device__ __forceinline__ uint32_t product_kind(bool bf16, bool b_by_n, int m, 
 // Map of a row-major rows x cols matrix of 16-bit values for copies of `box_rows` rows x 64 values, 128-byte swizzle, zeros
 // outside. False where the driver refuses it.
 bool tile_map(CUtensorMap *map, bool bf16, const void *base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
-
-// What the kernels that gave up have left behind: COMET_ERR_CUDA once, COMET_OK otherwise.
-inline comet_status_t tile_status(Context *ctx) {
-  volatile int32_t *word = ctx->h_pinned + kTileStatusWord;
-  if (!*word) return COMET_OK;
-  *word = 0;
-  return COMET_ERR_CUDA;
-}
 
 }  // namespace comet

@@ -34,6 +34,7 @@ template <class T> struct TileArgs {
   int nsrc, n, stages, act, bias_along;
   bool vec_out;
   int32_t *status;
+  int64_t patience;
 };
 
 // sum over row i's stored cells, column r, of one source
@@ -205,13 +206,15 @@ template <class T, int NACC, int kWords>
 __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const __grid_constant__ CUtensorMap map0, const __grid_constant__ CUtensorMap map1,
                                                                           const __grid_constant__ TileArgs<T> a) {
   extern __shared__ char raw_smem[];
-  __shared__ uint64_t bars[2 * 8 + 1];
+  __shared__ uint64_t bars[3 * 8 + 1];
   __shared__ uint32_t tmem_at;
   __shared__ int failed;
   char *smem = reinterpret_cast<char *>(((uintptr_t)raw_smem + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n = a.n, stages = a.stages, stage_bytes = NACC * kATile + kTileK * 2 * n;
-  const uint32_t full = smem_u32(bars), empty = full + 8 * stages, done = full + 16 * stages;
+  // Of a stage: A's tiles spread, B's tile landed, products done with both.
+  const uint32_t full = smem_u32(bars), landed = full + 8 * stages, empty = full + 16 * stages, done = full + 24 * stages;
+  int32_t issued = 0;                                          // copies, in the thread that issues them
   const int split = gridDim.z, rank = blockIdx.z;
   const int32_t from = (int32_t)((int64_t)a.steps * rank / split), to = (int32_t)((int64_t)a.steps * (rank + 1) / split);
   const int64_t row0 = (int64_t)blockIdx.x * kTileRows, col0 = (int64_t)blockIdx.y * n;
@@ -219,9 +222,10 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
   while (columns < (uint32_t)(NACC * n)) columns <<= 1;
 
   if (threadIdx.x == 0) {
-    failed = 0;
+    failed = a.patience <= 0;
     for (int s = 0; s < stages; ++s) {
-      bar_init(full + 8 * s, 4 * NACC + 1);
+      bar_init(full + 8 * s, 4 * NACC);
+      bar_init(landed + 8 * s, 1);
       bar_init(empty + 8 * s, 1);
     }
     bar_init(done, 1);
@@ -236,11 +240,11 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
   if (warp == 0) {
     if (lane == 0) {
       Place at;
-      for (int32_t t = from; t < to; ++t, at.next(stages)) {
-        if (at.round > 0 && !bar_wait(empty + 8 * at.stage, (at.round - 1) & 1, &failed)) break;
+      for (int32_t t = from; t < to; ++t, ++issued, at.next(stages)) {
+        if (at.round > 0 && !bar_wait(empty + 8 * at.stage, (at.round - 1) & 1, &failed, a.patience)) break;
         const bool second = t >= a.k_blocks;
         const int32_t block = second ? t - a.k_blocks : t;
-        const uint32_t bar = full + 8 * at.stage, b = smem_u32(smem + at.stage * stage_bytes + NACC * kATile);
+        const uint32_t bar = landed + 8 * at.stage, b = smem_u32(smem + at.stage * stage_bytes + NACC * kATile);
         bar_expect(bar, (uint32_t)(kTileK * 2 * n));
         for (int j = 0; j < n / 64; ++j) copy_box(b + j * (64 * kTileK * 2), second ? &map1 : &map0, (int)col0 + j * 64, block * kTileK, bar);
       }
@@ -250,7 +254,7 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
       const uint32_t kind = product_kind(Num<T>::is_bf16, true, kTileRows, n);
       Place at;
       for (int32_t t = from; t < to; ++t, at.next(stages)) {
-        if (!bar_wait(full + 8 * at.stage, at.round & 1, &failed)) break;
+        if (!bar_wait(landed + 8 * at.stage, at.round & 1, &failed, a.patience) || !bar_wait(full + 8 * at.stage, at.round & 1, &failed, a.patience)) break;
         tc_fence_after();
         const uint32_t tile = smem_u32(smem + at.stage * stage_bytes);
         const uint64_t b = operand_at(tile + NACC * kATile, 64 * kTileK * 2, 1024);
@@ -284,7 +288,7 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
         e.read(block, thread);
       }
       // (A wait that has run out does not leave the loop: the group's other warps may be at its barrier. From then on no wait takes time.)
-      const bool go = at.round == 0 || bar_wait_warp(empty + 8 * at.stage, (at.round - 1) & 1, &failed);
+      const bool go = at.round == 0 || bar_wait_warp(empty + 8 * at.stage, (at.round - 1) & 1, &failed, a.patience);
       const uint32_t tile = smem_u32(smem + at.stage * stage_bytes + q * kATile);
 #pragma unroll
       for (int k = 0; k < 8 && go; ++k)
@@ -302,7 +306,8 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
 
   // A spreading warp reads the accumulators of 32 rows (a lane each), each kParts-th group of 16 columns.
   __syncwarp();
-  const bool ok = bar_wait_warp(done, 0, &failed) && !__any_sync(0xffffffffu, failed);
+  const bool over = bar_wait_warp(done, 0, &failed, a.patience), ok = over && !__any_sync(0xffffffffu, failed);
+  if (warp == 1 && !over) bar_wait_end(done, 0);               // the products in flight, before tensor memory and stages go
   tc_fence_after();
   constexpr int kParts = (kTileWarps - 2) / 4;
   const int quarter = warp & 3, part = (warp - 2) >> 2;
@@ -399,7 +404,7 @@ __global__ void __launch_bounds__(kTileWarps * 32, 1) tile_product_kernel(const 
     }
     cluster.sync();                                     // nobody's shared memory goes while another reads it
   }
-  if (threadIdx.x == 0 && failed) give_up(full, stages, a.status);
+  if (threadIdx.x == 0 && failed) give_up(landed, stages, issued, a.status);
 }
 
 template <class T, int NACC, int kWords>
@@ -446,7 +451,8 @@ template <class T> comet_status_t product_typed(Context *ctx, const GatherCall &
   a.res = (const T *)c.residual;
   a.rows = (int32_t)c.src[0].A.rows;
   a.act = c.act; a.bias_along = c.bias_along;
-  a.status = ctx->h_pinned + kTileStatusWord;
+  a.status = ctx->h_pinned + kLayerStatusWord;
+  a.patience = wait_patience();
   a.k_blocks = (int32_t)ceil_div(c.src[0].A.cols, kTileK);
   const bool gated = c.mode == kGated;
   a.steps = c.mode == kSumOfTwo ? 2 * a.k_blocks : a.k_blocks;
@@ -495,8 +501,6 @@ bool tile_product_fits(int dtype, const GatherCall &c) {
 }
 
 comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &c, const TileList *lists, cudaStream_t s) {
-  const comet_status_t st = tile_status(ctx);
-  if (st != COMET_OK) return st;
   return dtype == COMET_BF16 ? product_typed<__nv_bfloat16>(ctx, c, lists, s) : product_typed<__half>(ctx, c, lists, s);
 }
 

@@ -17,6 +17,7 @@ template <class T> struct SampleTileArgs {
   T *out;
   int32_t rows, cols, k_blocks, n;
   int32_t *status;
+  int64_t patience;
 };
 
 template <class T>
@@ -32,10 +33,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
   const int stage_bytes = (kRows + n) * kK * 2;
   const uint32_t full = smem_u32(bars), empty = full + 8 * kStages, done = full + 16 * kStages;
   const int32_t row0 = (int32_t)blockIdx.x * kRows, col0 = (int32_t)blockIdx.y * n;
+  int32_t issued = 0;                                  // copies, in the thread that issues them
   uint32_t columns = 32;
   while (columns < (uint32_t)n) columns <<= 1;
   if (threadIdx.x == 0) {
-    failed = 0;
+    failed = a.patience <= 0;
     for (int s = 0; s < kStages; ++s) {
       bar_init(full + 8 * s, 1);
       bar_init(empty + 8 * s, 1);
@@ -51,9 +53,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
 
   if (warp == 0) {
     if (lane == 0) {
-      for (int32_t t = 0; t < a.k_blocks; ++t) {
+      for (int32_t t = 0; t < a.k_blocks; ++t, ++issued) {
         const int s = t % kStages, round = t / kStages;
-        if (round > 0 && !bar_wait(empty + 8 * s, (round - 1) & 1, &failed)) break;
+        if (round > 0 && !bar_wait(empty + 8 * s, (round - 1) & 1, &failed, a.patience)) break;
         const uint32_t p = smem_u32(smem + s * stage_bytes);
         bar_expect(full + 8 * s, (uint32_t)stage_bytes);
         copy_box(p, &map_p, t * kK, row0, full + 8 * s);
@@ -65,7 +67,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
       const uint32_t kind = product_kind(Num<T>::is_bf16, false, kRows, n);
       for (int32_t t = 0; t < a.k_blocks; ++t) {
         const int s = t % kStages, round = t / kStages;
-        if (!bar_wait(full + 8 * s, round & 1, &failed)) break;
+        if (!bar_wait(full + 8 * s, round & 1, &failed, a.patience)) break;
         tc_fence_after();
         const uint32_t p = smem_u32(smem + s * stage_bytes);
         const uint64_t x = operand_at(p, 16, 1024), y = operand_at(p + kRows * kK * 2, 16, 1024);
@@ -90,7 +92,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
   }
 
   __syncwarp();
-  const bool ok = bar_wait_warp(done, 0, &failed) && !__any_sync(0xffffffffu, failed);
+  const bool over = bar_wait_warp(done, 0, &failed, a.patience), ok = over && !__any_sync(0xffffffffu, failed);
+  if (warp == 1 && !over) bar_wait_end(done, 0);       // the products in flight, before tensor memory and stages go
   tc_fence_after();
   float *block = reinterpret_cast<float *>(smem);      // [n][kRows + 1]: the stages are free
   if (warp >= 2 && ok) {
@@ -133,7 +136,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) tile_sample_kernel(const __gri
     tc_fence_after();
     tmem_free(d, columns);
   }
-  if (threadIdx.x == 0 && failed) give_up(full, kStages, a.status);
+  if (threadIdx.x == 0 && failed) give_up(full, kStages, issued, a.status);
 }
 
 template <class T>
@@ -145,7 +148,8 @@ comet_status_t sample_tiles(Context *ctx, const RowView &A, const void *P, int64
   a.k_blocks = (int32_t)ceil_div(R, kK);
   const int64_t groups = ceil_div(A.cols, 64), tiles = ceil_div(groups, 4);
   a.n = (int)(ceil_div(groups, tiles) * 64);
-  a.status = ctx->h_pinned + kTileStatusWord;
+  a.status = ctx->h_pinned + kLayerStatusWord;
+  a.patience = wait_patience();
   CUtensorMap mp, mq;
   if (!tile_map(&mp, Num<T>::is_bf16, P, A.rows, R, ldp, kRows) || !tile_map(&mq, Num<T>::is_bf16, Q, A.cols, R, ldq, a.n)) return COMET_ERR_CUDA;
   const size_t ring = (size_t)kStages * (kRows + a.n) * kK * 2, block = (size_t)a.n * (kRows + 1) * sizeof(float);
@@ -167,8 +171,6 @@ bool tile_sample_fits(int dtype, const RowView &A, int64_t R) {
 
 comet_status_t tile_sample(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *Q, int64_t ldq, int64_t R, void *out,
                            cudaStream_t s) {
-  const comet_status_t st = tile_status(ctx);
-  if (st != COMET_OK) return st;
   return dtype == COMET_BF16 ? sample_tiles<__nv_bfloat16>(ctx, A, P, ldp, Q, ldq, R, out, s) : sample_tiles<__half>(ctx, A, P, ldp, Q, ldq, R, out, s);
 }
 
