@@ -150,12 +150,13 @@ comet_status_t sample_tiles(Context *ctx, const RowView &A, const void *P, int64
   a.n = (int)(ceil_div(groups, tiles) * 64);
   a.status = ctx->h_pinned + kLayerStatusWord;
   a.patience = wait_patience();
-  CUtensorMap mp, mq;
-  if (!tile_map(&mp, Num<T>::is_bf16, P, A.rows, R, ldp, kRows) || !tile_map(&mq, Num<T>::is_bf16, Q, A.cols, R, ldq, a.n)) return COMET_ERR_CUDA;
   const size_t ring = (size_t)kStages * (kRows + a.n) * kK * 2, block = (size_t)a.n * (kRows + 1) * sizeof(float);
   const size_t bytes = (ring > block ? ring : block) + 1024;
   auto *kernel = tile_sample_kernel<T>;
+  // (In front of the maps: their encoder wants a context, which a thread has from its first call of the runtime on.)
   COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  CUtensorMap mp, mq;
+  if (!tile_map(&mp, Num<T>::is_bf16, P, A.rows, R, ldp, kRows) || !tile_map(&mq, Num<T>::is_bf16, Q, A.cols, R, ldq, a.n)) return COMET_ERR_CUDA;
   kernel<<<dim3((unsigned)ceil_div(A.rows, kRows), (unsigned)tiles), kWarps * 32, bytes, s>>>(mp, mq, a);
   COMET_LAUNCH_CHECK(ctx);
   return COMET_OK;
