@@ -11,6 +11,8 @@ namespace {
 
 constexpr int kRows = 128, kK = 64, kWarps = 18;
 constexpr int kStages = 4;
+constexpr int kSampleSmem = kStages * (kRows + 256) * kK * 2 + 1024;   // most dynamic shared memory: blocks of 256 columns
+static_assert(256 * (kRows + 1) * (int)sizeof(float) + 1024 <= kSampleSmem, "the block of results takes the stages' place");
 
 template <class T> struct SampleTileArgs {
   const int32_t *pos, *crd;
@@ -154,7 +156,7 @@ comet_status_t sample_tiles(Context *ctx, const RowView &A, const void *P, int64
   const size_t bytes = (ring > block ? ring : block) + 1024;
   auto *kernel = tile_sample_kernel<T>;
   // (In front of the maps: their encoder wants a context, which a thread has from its first call of the runtime on.)
-  COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSampleSmem));      // the device's, not this call's
   CUtensorMap mp, mq;
   if (!tile_map(&mp, Num<T>::is_bf16, P, A.rows, R, ldp, kRows) || !tile_map(&mq, Num<T>::is_bf16, Q, A.cols, R, ldq, a.n)) return COMET_ERR_CUDA;
   kernel<<<dim3((unsigned)ceil_div(A.rows, kRows), (unsigned)tiles), kWarps * 32, bytes, s>>>(mp, mq, a);

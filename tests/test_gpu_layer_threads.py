@@ -71,3 +71,8 @@ class Threads:
 
 def test_the_first_call_of_a_thread(cuda_device, tmp_path):
     Threads(tmp_path, (256,), 1).run()
+
+
+def test_widths_beside_each_other(cuda_device, tmp_path):
+    """What a kernel may take of shared memory belongs to the device, not to a call: narrow blocks must not take it from the wide ones beside them."""
+    Threads(tmp_path, (64, 256, 128, 256, 192, 64), 20_000).run()
