@@ -684,7 +684,8 @@ static comet_status_t launch_dot(Context *ctx, SegDotArgs a, cudaStream_t stream
 #define COMET_RES_IPT 5
 #endif
 constexpr int kResVC = COMET_RES_VC, kResThreads = COMET_RES_THREADS, kResIpt = COMET_RES_IPT;
-constexpr size_t kMaxDynamicSmem = 232448;               // 227 KB opt-in limit per CTA on sm_100
+constexpr size_t kMaxDynamicSmem = 232448;               // 227 KB opt-in limit per CTA on sm_100 (a kernel's limit is the device's, not a call's:
+                                                         // always all of it, since calls on other handles run beside this one)
 
 template <class T>
 static comet_status_t launch_resident(Context *ctx, SegDotArgs a, int64_t x_len, cudaStream_t stream) {
@@ -705,7 +706,7 @@ static comet_status_t launch_resident(Context *ctx, SegDotArgs a, int64_t x_len,
   const int32_t x_bytes = (int32_t)align_up((size_t)x_len * sizeof(T), 16);
   const size_t smem = (size_t)x_bytes + (size_t)kResVC * RL::kStageBytes;
   auto kernel = seg_dot_resident_kernel<T, kResVC, kResThreads, kResIpt>;
-  COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxDynamicSmem));
   const int64_t ctas = ceil_div(a.num_tiles, kResVC) < kSmCount ? ceil_div(a.num_tiles, kResVC) : kSmCount;
   kernel<<<(unsigned)ctas, kResVC * kResThreads, smem, stream>>>(a, splits, x_len, x_bytes);
   COMET_LAUNCH_CHECK(ctx);
@@ -743,7 +744,7 @@ static comet_status_t launch_stream(Context *ctx, SegDotArgs a, int64_t x_len, b
     unsigned int *ctas_done = reinterpret_cast<unsigned int *>(ctx->d_status + 34);
     if (xsmem) {
       auto kernel = seg_dot_stream2_kernel<T, true>;
-      COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)x_bytes));
+      COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxDynamicSmem));
       kernel<<<(unsigned)ctas, 1024, x_bytes, stream>>>(a, x_len, (int32_t)span, next_tile, ctas_done);
     } else {
       seg_dot_stream2_kernel<T, false><<<(unsigned)ctas, 1024, 0, stream>>>(a, x_len, (int32_t)span, next_tile, ctas_done);
@@ -757,7 +758,7 @@ static comet_status_t launch_stream(Context *ctx, SegDotArgs a, int64_t x_len, b
   COMET_CUDA_TRY(ctx, cudaMemsetAsync(next_tile, 0, sizeof(unsigned long long), stream));
   if (xsmem) {
     auto kernel = seg_dot_stream_kernel<T, true>;
-    COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)x_bytes));
+    COMET_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxDynamicSmem));
     kernel<<<(unsigned)ctas, 1024, x_bytes, stream>>>(a, x_len, (int32_t)span, next_tile);
   } else {
     seg_dot_stream_kernel<T, false><<<(unsigned)ctas, 1024, 0, stream>>>(a, x_len, (int32_t)span, next_tile);

@@ -404,7 +404,7 @@ static comet_status_t entries_hot(Context *ctx, const ScatterArgs &a, bool coo, 
     }
     auto kernel = coo ? mttkrp_csf_leaf_hot_kernel<T, true> : mttkrp_csf_leaf_hot_kernel<T, false>;
     const size_t smem = (size_t)slots * a.R * sizeof(double);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kHotBytes);      // the device's, not this call's
     if (e != cudaSuccess) st = cuda_fail(ctx, e);
     if (st == COMET_OK) {
       kernel<<<kHotCtas * kSmCount, kHotThreads, smem, stream>>>(a, fiber_root, hot_slot, hot_rows, n_hot, (int32_t)slots,

@@ -22,11 +22,17 @@ static void *run(void *arg) {
   for (int64_t k = 0; k < j->times; ++k) j->refused += j->call(j->handle, j->a, j->p, j->r, j->q, j->r, j->r, j->out, j->stream) != 0;
   return 0;
 }
-int hammer(struct job *jobs, int n) {
+typedef int (*spmv_t)(void *, const void *, const void *, void *, void *);
+static void *run_spmv(void *arg) {
+  struct job *j = arg;
+  for (int64_t k = 0; k < j->times; ++k) j->refused += ((spmv_t)j->call)(j->handle, j->a, j->p, j->out, j->stream) != 0;
+  return 0;
+}
+int hammer(struct job *jobs, int n, int spmv) {
   pthread_t t[16];
   int started = 0;
   for (; started < n && started < 16; ++started)
-    if (pthread_create(t + started, 0, run, jobs + started)) break;
+    if (pthread_create(t + started, 0, spmv ? run_spmv : run, jobs + started)) break;
   for (int i = 0; i < started; ++i) pthread_join(t[i], 0);
   return started;
 }
@@ -39,18 +45,26 @@ class Job(C.Structure):
 
 
 class Threads:
-    """A thread for each of some sampled products of 64 columns, each with a handle (without an allocator: nothing goes through Python) and a stream of its own."""
+    """A thread for each of some sampled products of 64 columns, or products with a vector, each with a handle (without an allocator: nothing goes through Python) and a stream of its own."""
 
-    def __init__(self, tmp_path, widths, times):
+    def __init__(self, tmp_path, widths, times, spmv=False):
+        self.spmv = spmv
         (tmp_path / "hammer.c").write_text(SOURCE)
         subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-pthread", "-o", str(tmp_path / "hammer.so"), str(tmp_path / "hammer.c")], check=True)
         self.hammer = C.CDLL(str(tmp_path / "hammer.so")).hammer
         self.lib, self.keep, self.jobs = comet.load_library(), [], (Job * len(widths))()
         rng = np.random.default_rng(0)
         for job, cols in zip(self.jobs, widths):
-            m = Matrix(random_mask(256, cols, 0.3, rng), torch.bfloat16, rng)
+            m = Matrix(random_mask(256, cols, 0.3, rng), torch.float64 if spmv else torch.bfloat16, rng)
             handle, stream = C.c_void_p(), torch.cuda.Stream()
             assert self.lib.comet_create(C.byref(handle), None) == 0
+            if spmv:
+                x, out = torch.randn(cols, dtype=torch.float64, device="cuda"), torch.zeros(256, dtype=torch.float64, device="cuda")
+                want = comet.spmv(m.t, x).clone()
+                job.call, job.handle, job.a, job.p = C.cast(self.lib.comet_spmv, C.c_void_p), handle, C.addressof(m.t.c), x.data_ptr()
+                job.out, job.stream, job.times = out.data_ptr(), stream.cuda_stream, times
+                self.keep.append((m, handle, stream, x, out, want))
+                continue
             P, Q = torch.randn(256, 64, device="cuda").bfloat16(), torch.randn(cols, 64, device="cuda").bfloat16()
             out = torch.zeros(m.t.nnz, dtype=torch.bfloat16, device="cuda")
             want = comet.sddmm(m.t, P, Q).val.clone()
@@ -61,7 +75,7 @@ class Threads:
         torch.cuda.synchronize()
 
     def run(self):
-        assert self.hammer(self.jobs, len(self.jobs)) == len(self.jobs)
+        assert self.hammer(self.jobs, len(self.jobs), self.spmv) == len(self.jobs)
         torch.cuda.synchronize()
         assert [j.refused for j in self.jobs] == [0] * len(self.jobs)
         for m, handle, *_, out, want in self.keep:
@@ -76,3 +90,10 @@ def test_the_first_call_of_a_thread(cuda_device, tmp_path):
 def test_widths_beside_each_other(cuda_device, tmp_path):
     """What a kernel may take of shared memory belongs to the device, not to a call: narrow blocks must not take it from the wide ones beside them."""
     Threads(tmp_path, (64, 256, 128, 256, 192, 64), 20_000).run()
+
+
+@pytest.mark.parametrize("kernel", ["stream", "stream2", "resident"])
+def test_spmv_of_different_lengths(cuda_device, tmp_path, monkeypatch, kernel):
+    """The same of comet_spmv, whose vectors lie in shared memory: 128 KB of it, or next to none."""
+    monkeypatch.setenv("COMET_SEG_DOT_KERNEL", kernel)
+    Threads(tmp_path, (64, 16_000, 300, 15_000, 9000, 64), 10_000, spmv=True).run()
