@@ -176,6 +176,7 @@ comet_status_t layer_sample(Context *ctx, int dtype, const RowView &A, const voi
 
 // A matrix's entries by tiles of 128 x 64 (layer_tile_list.cu; its rows have to be ordered): words of tile (t, b) at words + bases[t * (blocks + 1) + b] up to the next base.
 struct TileList { const uint32_t *words; const int32_t *bases; };
+bool tile_lists_fit(const RowView &A);
 size_t tile_list_bytes(const RowView &A);
 comet_status_t tile_lists(Context *ctx, const RowView *A, const int32_t *const *pick, int sources, char *const *mem, TileList *lists, cudaStream_t s);
 

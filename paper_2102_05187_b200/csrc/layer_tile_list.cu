@@ -141,6 +141,8 @@ struct ListSizes {
 
 }  // namespace
 
+bool tile_lists_fit(const RowView &A) { return A.cols <= (65535ll * 32 - 1) * 64; }      // 32 starts of blocks of 64 columns for each blockIdx.y
+
 size_t tile_list_bytes(const RowView &A) {
   const ListSizes z(A);
   return z.words + z.starts + z.bases;
@@ -159,9 +161,11 @@ comet_status_t tile_lists(Context *ctx, const RowView *A, const int32_t *const *
   }
   const dim3 rows((unsigned)ceil_div(a.rows, kListWarps), (unsigned)sources);
   tile_starts_kernel<<<rows, kListThreads, 0, s>>>(a);
+  COMET_LAUNCH_CHECK(ctx);                                 // each pass trusts what the one before it wrote
   tile_shifts_kernel<<<dim3((unsigned)ceil_div(a.rows, 128), (unsigned)ceil_div(a.k_blocks + 1, 32), (unsigned)sources), kListThreads, 0, s>>>(a);
+  COMET_LAUNCH_CHECK(ctx);
   tile_words_kernel<<<rows, kListThreads, 0, s>>>(a);
-  COMET_LAUNCHED(ctx, 3);
+  COMET_LAUNCH_CHECK(ctx);
   return COMET_OK;
 }
 

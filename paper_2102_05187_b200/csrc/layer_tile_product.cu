@@ -488,12 +488,12 @@ static double least_work() {
 
 bool tile_product_fits(int dtype, const GatherCall &c) {
   if (dtype != COMET_BF16 && dtype != COMET_F16) return false;
-  if (c.R < 8 || c.R >= (1ll << 24)) return false;
+  if (c.R < 8 || c.R > 65535ll * 64) return false;         // column tiles are counted by blockIdx.y
   const int n = c.mode == kLayer ? 1 : 2;
   double nnz = 0, cells = 0;
   for (int q = 0; q < n; ++q) {
     const GatherSource &g = c.src[q];
-    if (!g.A.ordered) return false;
+    if (!g.A.ordered || !tile_lists_fit(g.A)) return false;
     nnz += (double)g.A.nnz;
     cells += (double)g.A.rows * (double)g.A.cols;
   }
