@@ -336,8 +336,13 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  *     cudaErrorLaunchTimeout as its comet_last_cuda_error) and launches nothing, and the one after it works again. Calls captured into a graph
  *     report in the same way, to the next call made outside of it.
  *   - Which kernels a call takes follows from types, sizes and the share of stored cells: up to 16 bytes of columns read B from shared
- *     memory; 16-bit matrices with at least 1/64 of their cells stored run on the tensor cores (8 columns and more, enough work), where about
- *     8 bytes of temporary memory per entry are taken; short rows go through the kernels of comet_spmm, 16-bit operands as fp32 copies.
+ *     memory; 16-bit matrices with at least 1/64 of their cells stored run on the tensor cores (8 columns and more, enough work); short
+ *     rows go through the kernels of comet_spmm, 16-bit operands as fp32 copies.
+ *   - Temporary memory: the lists of the tensor-core product take 4 bytes per entry and 8 per row and block of 64 columns of A (one block more,
+ *     and rounded up to 8 blocks: at 1/64 of the cells 12 bytes per entry in wide matrices, 68 in one of 64 columns); operands whose rows do not start on 16 bytes are copied where
+ *     that pays; the copies in fp32 take 4 bytes per value of A, B and C. A product that gets none of this from the allocator falls back to
+ *     kernels that need no memory. COMET_ERR_ALLOC is left for what there is no form without: row boundaries, the values of a
+ *     transposed matrix in its order, dZ, column sums.
  */
 typedef enum { COMET_ACT_NONE = 0, COMET_ACT_RELU = 1, COMET_ACT_GELU = 2 /* with erf */, COMET_ACT_GELU_TANH = 3, COMET_ACT_SILU = 4 } comet_act_t;
 typedef enum { COMET_BIAS_ROWS = 0, COMET_BIAS_COLS = 1 } comet_bias_t;

@@ -73,7 +73,7 @@ struct Temps {
 };
 
 // A dense operand of the products whose rows do not start on 16 bytes is copied into padded rows where that pays: always for the tensor-core forms,
-// which cannot do without, and for gathers of rows of several pieces where the entries gather it more than a few times over.
+// which cannot do without (they are left to the others where there is no room for it), and for gathers of rows of several pieces where the entries gather it more than a few times over.
 // (Graph matrix of 3.2 M entries, 50 columns of fp32: the call 474 us with gathers of single values, 275 us with the copy, which is 17 of them.)
 comet_status_t pad_operand(Context *ctx, int dtype, const void *&B, int64_t &ldb, int64_t rows, int64_t R, Temps &temps) {
   const int64_t ld = layer_padded(dtype, R);
@@ -184,18 +184,18 @@ comet_status_t pick_values(Context *ctx, int dtype, GatherSource &g, Temps &temp
   return st;
 }
 
-comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
-  if (c.src[0].A.rows == 0) return COMET_OK;
-  const int n = c.mode == kLayer ? 1 : 2;
-  const bool panel = panel_fits(dtype, c), tiles = !panel && tile_product_fits(dtype, c), apart = !panel && !tiles && apart_fits(dtype, c);
-  for (int q = 0; q < n && !tiles; ++q) {
-    if (!c.src[q].pick || (apart && layer_elem_size(dtype) == 2)) continue;          // widened by number there
+comet_status_t pick_values(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
+  for (int q = 0; q < (c.mode == kLayer ? 1 : 2); ++q) {
+    if (!c.src[q].pick) continue;
     const comet_status_t st = pick_values(ctx, dtype, c.src[q], temps);
     if (st != COMET_OK) return st;
   }
-  if (panel) return layer_panel(ctx, dtype, c, temps.s);
-  if (apart) return product_apart(ctx, dtype, c, temps);
-  for (int q = 0; q < n; ++q) {
+  return COMET_OK;
+}
+
+// Copies of operands whose rows do not start on 16 bytes: of all (tiles), or where gathers pay for them.
+comet_status_t pad_operands(Context *ctx, int dtype, GatherCall &c, bool all, Temps &temps) {
+  for (int q = 0; q < (c.mode == kLayer ? 1 : 2); ++q) {
     GatherSource &g = c.src[q];
     if (layer_aligned(dtype, g.B, g.ldb)) continue;
     if (q == 1 && c.mode == kGated) {                       // one operand for both matrices
@@ -203,11 +203,17 @@ comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
       g.ldb = c.src[0].ldb;
       continue;
     }
-    if (!tiles && !gathers_pay_padding(dtype, g.A.nnz, g.A.cols, c.R)) continue;
+    if (!all && !gathers_pay_padding(dtype, g.A.nnz, g.A.cols, c.R)) continue;
     const comet_status_t st = pad_operand(ctx, dtype, g.B, g.ldb, g.A.cols, c.R, temps);
     if (st != COMET_OK) return st;
   }
-  if (!tiles) return layer_gather(ctx, dtype, c, temps.s);
+  return COMET_OK;
+}
+
+comet_status_t product_tiles(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
+  comet_status_t st = pad_operands(ctx, dtype, c, true, temps);
+  if (st != COMET_OK) return st;
+  const int n = c.mode == kLayer ? 1 : 2;
   RowView A[2];
   const int32_t *pick[2];
   char *mem[2];
@@ -218,21 +224,39 @@ comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
     mem[q] = (char *)temps.get(tile_list_bytes(A[q]));
     if (!mem[q]) return COMET_ERR_ALLOC;
   }
-  const comet_status_t st = tile_lists(ctx, A, pick, n, mem, lists, temps.s);
+  st = tile_lists(ctx, A, pick, n, mem, lists, temps.s);
   return st != COMET_OK ? st : tile_product(ctx, dtype, c, lists, temps.s);
+}
+
+// A form that finds no room for its lists or copies leaves the product to the workers per row, which need none (but for the values of a transposed matrix, which
+// all but the tiles want in its own order). What it has written by then is written again.
+comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
+  if (c.src[0].A.rows == 0) return COMET_OK;
+  const bool panel = panel_fits(dtype, c);
+  comet_status_t st = COMET_ERR_ALLOC;
+  if (!panel && tile_product_fits(dtype, c)) {
+    if ((st = product_tiles(ctx, dtype, c, temps)) != COMET_ERR_ALLOC) return st;
+  } else if (!panel && apart_fits(dtype, c)) {
+    if (layer_elem_size(dtype) != 2 && (st = pick_values(ctx, dtype, c, temps)) != COMET_OK) return st;       // 16 bits: widened by number
+    if ((st = product_apart(ctx, dtype, c, temps)) != COMET_ERR_ALLOC) return st;
+  }
+  if ((st = pick_values(ctx, dtype, c, temps)) != COMET_OK) return st;
+  if (panel) return layer_panel(ctx, dtype, c, temps.s);
+  st = pad_operands(ctx, dtype, c, false, temps);
+  return st != COMET_OK && st != COMET_ERR_ALLOC ? st : layer_gather(ctx, dtype, c, temps.s);
 }
 
 // (Q is left padded where it was copied, for a second call on it.)
 comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *&Q, int64_t &ldq, int64_t R, void *out, Temps &temps) {
   const bool tiles = tile_sample_fits(dtype, A, R);
-  const bool pad_p = !layer_aligned(dtype, P, ldp), pad_q = !layer_aligned(dtype, Q, ldq);
+  comet_status_t st = COMET_OK;
   if (tiles || gathers_pay_padding(dtype, A.nnz, A.rows + A.cols, R)) {
-    comet_status_t st = COMET_OK;
-    if (pad_p) st = pad_operand(ctx, dtype, P, ldp, A.rows, R, temps);
-    if (st == COMET_OK && pad_q) st = pad_operand(ctx, dtype, Q, ldq, A.cols, R, temps);
-    if (st != COMET_OK) return st;
+    if (!layer_aligned(dtype, P, ldp)) st = pad_operand(ctx, dtype, P, ldp, A.rows, R, temps);
+    if (st == COMET_OK && !layer_aligned(dtype, Q, ldq)) st = pad_operand(ctx, dtype, Q, ldq, A.cols, R, temps);
+    if (st != COMET_OK && st != COMET_ERR_ALLOC) return st;
   }
-  return tiles ? tile_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s) : layer_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s);
+  // no room for a copy: the gathers take operands as they are
+  return tiles && st == COMET_OK ? tile_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s) : layer_sample(ctx, dtype, A, P, ldp, Q, ldq, R, out, temps.s);
 }
 
 // What a kernel of an earlier call has left behind that gave up: COMET_ERR_CUDA once, COMET_OK otherwise.

@@ -368,12 +368,15 @@ comet_status_t gather_launch(Context *ctx, GatherArgs<T> &a, int64_t nnz, bool h
   typename Num<T>::sum *part = nullptr;
   char *mem = nullptr;
   cudaError_t e = cudaSuccess;
+  // at most nnz / kHugeRow rows, with an item for each kHugeItem entries and at most one more per source
+  const int64_t max_rows = nnz / kHugeRow, max_items = nnz / kHugeItem + 2 * max_rows;
+  const size_t b_items = align_up((size_t)max_items * sizeof(HugeItem), 256), b_rows = align_up((size_t)max_rows * sizeof(HugeRow), 256);
+  if (huge) mem = (char *)ctx_alloc(ctx, 256 + b_items + b_rows + (size_t)max_items * (size_t)a.R * sizeof(*part), s);
+  if (!mem) {                            // none, or no room for them: they are rows like the other long ones
+    huge = false;
+    a.huge_len = 2147483647;
+  }
   if (huge) {
-    // at most nnz / kHugeRow rows, with an item for each kHugeItem entries and at most one more per source
-    const int64_t max_rows = nnz / kHugeRow, max_items = nnz / kHugeItem + 2 * max_rows;
-    const size_t b_items = align_up((size_t)max_items * sizeof(HugeItem), 256), b_rows = align_up((size_t)max_rows * sizeof(HugeRow), 256);
-    mem = (char *)ctx_alloc(ctx, 256 + b_items + b_rows + (size_t)max_items * (size_t)a.R * sizeof(*part), s);
-    if (!mem) return COMET_ERR_ALLOC;
     counts = (int32_t *)mem;
     items = (HugeItem *)(mem + 256);
     rows = (HugeRow *)(mem + 256 + b_items);
