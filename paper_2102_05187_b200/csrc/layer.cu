@@ -72,9 +72,7 @@ struct Temps {
   }
 };
 
-// A dense operand of the products whose rows do not start on 16 bytes is copied into padded rows where that pays: always for the tensor-core forms,
-// which cannot do without (they are left to the others where there is no room for it), and for gathers of rows of several pieces where the entries gather it more than a few times over.
-// (Graph matrix of 3.2 M entries, 50 columns of fp32: the call 474 us with gathers of single values, 275 us with the copy, which is 17 of them.)
+// A copy of a dense operand into rows that start on 16 bytes, which the tensor-core forms cannot do without.
 comet_status_t pad_operand(Context *ctx, int dtype, const void *&B, int64_t &ldb, int64_t rows, int64_t R, Temps &temps) {
   const int64_t ld = layer_padded(dtype, R);
   void *copy = temps.get((size_t)rows * (size_t)ld * layer_elem_size(dtype));
@@ -84,6 +82,10 @@ comet_status_t pad_operand(Context *ctx, int dtype, const void *&B, int64_t &ldb
   ldb = ld;
   return st;
 }
+// The sampled product by gathers reads both operands' rows once per entry, in pieces of 16 bytes or value by value: a copy pays from a few entries per row and some
+// pieces on (fp32, 1.7 M entries, 50 columns 153 us against 192; 6.7 M, 129 columns 1,144 against 2,201; 0.3 M, 50 columns the same). The products by a
+// worker per row hide single values behind their many entries in flight, and a copy only costs them (1.7 M entries in 4,096 rows, fp32, 50 columns 59 us, with
+// one 78; bf16, 17 columns 40 and 55; 6.7 M, fp32, 129 columns 709 and 694).
 bool gathers_pay_padding(int dtype, int64_t nnz, int64_t rows, int64_t R) {
   return nnz >= 100000 && nnz >= 4 * rows && R * (int64_t)layer_elem_size(dtype) >= 32;
 }
@@ -193,8 +195,8 @@ comet_status_t pick_values(Context *ctx, int dtype, GatherCall &c, Temps &temps)
   return COMET_OK;
 }
 
-// Copies of operands whose rows do not start on 16 bytes: of all (tiles), or where gathers pay for them.
-comet_status_t pad_operands(Context *ctx, int dtype, GatherCall &c, bool all, Temps &temps) {
+comet_status_t product_tiles(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
+  comet_status_t st = COMET_OK;
   for (int q = 0; q < (c.mode == kLayer ? 1 : 2); ++q) {
     GatherSource &g = c.src[q];
     if (layer_aligned(dtype, g.B, g.ldb)) continue;
@@ -203,16 +205,8 @@ comet_status_t pad_operands(Context *ctx, int dtype, GatherCall &c, bool all, Te
       g.ldb = c.src[0].ldb;
       continue;
     }
-    if (!all && !gathers_pay_padding(dtype, g.A.nnz, g.A.cols, c.R)) continue;
-    const comet_status_t st = pad_operand(ctx, dtype, g.B, g.ldb, g.A.cols, c.R, temps);
-    if (st != COMET_OK) return st;
+    if ((st = pad_operand(ctx, dtype, g.B, g.ldb, g.A.cols, c.R, temps)) != COMET_OK) return st;
   }
-  return COMET_OK;
-}
-
-comet_status_t product_tiles(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
-  comet_status_t st = pad_operands(ctx, dtype, c, true, temps);
-  if (st != COMET_OK) return st;
   const int n = c.mode == kLayer ? 1 : 2;
   RowView A[2];
   const int32_t *pick[2];
@@ -241,9 +235,7 @@ comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
     if ((st = product_apart(ctx, dtype, c, temps)) != COMET_ERR_ALLOC) return st;
   }
   if ((st = pick_values(ctx, dtype, c, temps)) != COMET_OK) return st;
-  if (panel) return layer_panel(ctx, dtype, c, temps.s);
-  st = pad_operands(ctx, dtype, c, false, temps);
-  return st != COMET_OK && st != COMET_ERR_ALLOC ? st : layer_gather(ctx, dtype, c, temps.s);
+  return panel ? layer_panel(ctx, dtype, c, temps.s) : layer_gather(ctx, dtype, c, temps.s);
 }
 
 // (Q is left padded where it was copied, for a second call on it.)

@@ -85,3 +85,19 @@ def test_the_transposed_product_without_memory_for_its_form(cuda_device, kind, t
     h.arm(None)
     bound = (m.tallest + 8) * 2.0 ** -24 * N
     assert bool(((dB - want).abs() <= bound + torch.finfo(dt).eps / 2 * (want.abs() + bound) + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("dtype,rows,cols,density,R", [("f32", 512, 1000, 0.4, 50), ("f32", 300, 1500, 0.3, 129), ("f16", 512, 1000, 0.4, 17)])
+def test_workers_per_row_take_operands_as_they_are(cuda_device, dtype, rows, cols, density, R):
+    """One launch, no copy of rows that do not start on 16 bytes, no temporary memory."""
+    dt = TYPES[dtype]
+    rng = np.random.default_rng(9)
+    h = FailingHandle()
+    m, u = (Matrix(random_mask(rows, cols, density, rng), dt, rng, scale=0.05) for _ in range(2))
+    m.t.handle = u.t.handle = h
+    h.arm(None)
+    for check in (lambda: check_epilogue(m, dt, R, "gelu", "rows", True, True, rng), lambda: check_gated(m, u, dt, R, "silu", True, rng)):
+        before = h.kernel_launches()
+        check()
+        assert h.kernel_launches() - before == 1
+    assert h.calls == 0
