@@ -238,8 +238,8 @@ comet_status_t product(Context *ctx, int dtype, GatherCall &c, Temps &temps) {
   return panel ? layer_panel(ctx, dtype, c, temps.s) : layer_gather(ctx, dtype, c, temps.s);
 }
 
-// (Q is left padded where it was copied, for a second call on it.)
-comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *P, int64_t ldp, const void *&Q, int64_t &ldq, int64_t R, void *out, Temps &temps) {
+// (P and Q are left padded where they were copied, for a second call on them.)
+comet_status_t sampled(Context *ctx, int dtype, const RowView &A, const void *&P, int64_t &ldp, const void *&Q, int64_t &ldq, int64_t R, void *out, Temps &temps) {
   const bool tiles = tile_sample_fits(dtype, A, R);
   comet_status_t st = COMET_OK;
   if (tiles || gathers_pay_padding(dtype, A.nnz, A.rows + A.cols, R)) {
@@ -538,7 +538,9 @@ extern "C" comet_status_t comet_spmm_gated_backward(comet_handle_t handle, const
     if (!dval || A->nnz == 0) continue;
     RowView v;
     st = view_rows(ctx, A, temps, &v);
-    if (st == COMET_OK) st = sampled(ctx, G->dtype, v, g.dz[q], g.lddz, B, ldb, R, dval, temps);
+    const void *dz = g.dz[q];
+    int64_t lddz = g.lddz;
+    if (st == COMET_OK) st = sampled(ctx, G->dtype, v, dz, lddz, B, ldb, R, dval, temps);
     if (st != COMET_OK) return st;
   }
   if (!dB) return COMET_OK;

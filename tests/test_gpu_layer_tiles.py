@@ -177,3 +177,19 @@ def test_only_stored_cells_count_in_tiles(cuda_device, any_work, dtype, cols, R,
     want = (mt.dense + ut.dense).t() @ B64
     N = (mt.dense.abs() + ut.dense.abs()).t() @ B64.abs()
     others(dB, want, stored(dt, want, z_bound(dt, mt.tallest + ut.tallest, N, want)), "sum of two")
+
+
+def test_one_copy_of_a_gradient_for_both_of_its_products(cuda_device, any_work):
+    """Without an activation dZ is dC itself: where its rows do not start on 16 bytes it is copied once, for dval and dB."""
+    dt = torch.bfloat16
+    rng = np.random.default_rng(4)
+    m = Matrix(random_mask(300, 400, 0.3, rng), dt, rng, scale=0.1)
+    (B, B64), (dC, dC64) = values((400, 61), dt, rng), values((300, 61), dt, rng)
+    At, B, dC = comet.transpose_symbolic(m.t), B.cuda(), dC.cuda()
+    with Launches(COPY + COPY + 1 + LISTS + PRODUCT):      # dC, B, the sampled product, dB
+        dval, dB, _ = comet.spmm_epilogue_backward(m.t, At, B, dC)
+    r, c = m.rc
+    want, N = (dC64[r] * B64[c]).sum(1), (dC64[r].abs() * B64[c].abs()).sum(1)
+    assert_within(dval, want, stored(dt, want, 71 * u_of(dt) * N), "dval")
+    want, N = m.dense.t() @ dC64, m.dense.abs().t() @ dC64.abs()
+    assert_within(dB, want, stored(dt, want, z_bound(dt, m.tallest, N, want)), "dB")
