@@ -87,7 +87,8 @@ typedef enum {
  *   COMET_MTTKRP_HOT_ROWS=0|1   per-entry MTTKRP (CSF leaf mode, COO non-root modes): never / always keep the most popular output rows in shared memory
  *                               (default: for R >= 16 and at least 2^20 entries)
  *   COMET_HOST_CHUNK_BYTES=n    comet_spmm_from_host: bytes per row of a column chunk of B and C (default 256; 0 = one chunk)
- *   COMET_LAYER_TILE_WORK=n     layer operators: entries x columns from which 16-bit products run on the tensor cores (default 40000000)
+ *   COMET_LAYER_TILE_WORK=n     layer operators: entries x columns from which 16-bit products run on the tensor cores, whatever the number of columns
+ *                               (default 40000000, and as many as the matrix has cells, from 20 columns on)
  *   COMET_LAYER_WAIT_CYCLES=n   layer operators: cycles after which a wait of the tensor-core kernels gives up (default 8000000000; 0: at once)
  *   COMET_SPMM_LONG_ROWS=0      comet_spmm without the long-row path; COMET_SPMM_LONG_ROW, _LONG_TILE, _PIECE,
  *                               _BLOCK_MB, _BLOCKS, _LONG_CTAS, _LONG_MIN_NNZ, _LONG_MIN_B_MB: its threshold
@@ -336,8 +337,9 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  *     cudaErrorLaunchTimeout as its comet_last_cuda_error) and launches nothing, and the one after it works again. Calls captured into a graph
  *     report in the same way, to the next call made outside of it.
  *   - Which kernels a call takes follows from types, sizes and the share of stored cells: up to 16 bytes of columns read B from shared
- *     memory; 16-bit matrices with at least 1/64 of their cells stored run on the tensor cores (8 columns and more, enough work); short
- *     rows go through the kernels of comet_spmm, 16-bit operands as fp32 copies.
+ *     memory (rows of 48 entries and more on average); 16-bit matrices with at least 1/64 of their cells stored run on the tensor cores (20
+ *     columns and more, enough work), sampled products from 1/128 and one entry x column per cell on; short rows go through the kernels of
+ *     comet_spmm, 16-bit operands as fp32 copies.
  *   - Temporary memory: the lists of the tensor-core product take 4 bytes per entry and 8 per row and block of 64 columns of A (one block more,
  *     and rounded up to 8 blocks: at 1/64 of the cells 12 bytes per entry in wide matrices, 68 in one of 64 columns); operands whose rows do not start on 16 bytes are copied where
  *     that pays; the copies in fp32 take 4 bytes per value of A, B and C. A product that gets none of this from the allocator falls back to

@@ -18,7 +18,11 @@ template <class T> comet_status_t layer_gather_typed(Context *ctx, const GatherC
 template <class T> comet_status_t layer_panel_typed(Context *ctx, const GatherCall &c, cudaStream_t s);    // layer_panel.cuh, likewise
 
 // A few columns of matrices whose entries are worth laying B down in every SM's shared memory: rows of B of up to 16 bytes, no more of
-// them (148 times) than the matrix has bytes, and no row more than 64 times as long as the mean; ordered rows where it takes several panels.
+// them (148 times) than the matrix has bytes, 1/64 of the cells (no row is more than 64 times as long as the mean then), and rows of 48 entries on average, since a row
+// has a warp of its own; ordered rows where it takes several panels. Measured, panels and the other forms, us: 100,000 rows of 250 entries, one column of bf16 49
+// and 79, of 62 entries 36 and 32, of 31 34 and 20; eight columns 121 and 324, 94 and 239, 90 and 62; one column of fp32 53 and 74, 39 and 32, 36
+// and 20; four 87 and 142, 62 and 121, 59 and 68; 300,000 rows of 16 entries, one column of bf16 86 and 28, eight 247 and 83. With 4096 columns of A 1/64 of the
+// cells are rows of 64 entries: 13 us either way.
 bool panel_fits(int dtype, const GatherCall &c) {
   const double es = (double)layer_elem_size(dtype);
   if ((double)c.R * es > 16.0) return false;
@@ -31,7 +35,7 @@ bool panel_fits(int dtype, const GatherCall &c) {
     nnz += (double)c.src[q].A.nnz;
     cells += (double)c.src[q].A.rows * (double)c.src[q].A.cols;
   }
-  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz * (4 + es) >= kSmCount * (double)c.src[0].A.cols * (double)c.R * es;
+  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz >= 48.0 * n * (double)c.src[0].A.rows && nnz * (4 + es) >= kSmCount * (double)c.src[0].A.cols * (double)c.R * es;
 }
 comet_status_t layer_panel(Context *ctx, int dtype, const GatherCall &c, cudaStream_t s) {
   switch (dtype) {
@@ -99,6 +103,10 @@ bool apart_fits(int dtype, const GatherCall &c) {
   const bool plain = c.mode == kLayer && c.act == COMET_ACT_NONE && !c.src[0].bias && !c.src[0].pre && !c.residual;
   // Rows of some length keep a worker of their own busy, and its epilogue costs nothing: 1.7 M entries in 4,096 rows, 32 columns of fp32 33 us against
   // 44, 16 of bf16 29 against 49; but 0.8 M entries, 100 columns of fp64 197 against 79.
+  // Short rows: what decides is how even they are, which the host does not know. The numbers of entries lie between the two. Apart and by rows, fp32, us: power-law
+  // rows, 0.17 M entries, 8 columns 27 and 28 (a layer 31 and 28, a pair 57 and 40), 50 columns 24 and 71 (30 and 72, 53 and 102); 0.42 M, 8 columns 31 and 46 (36 and 47, 68
+  // and 78), 50 columns 37 and 126; even rows of 20, 0.16 M, 8 columns 20 and 12, 50 columns 18 and 24 (24 and 26, 41 and 36); 0.32 M, 8 columns 22 and 12 (25 and 13, 47 and 14),
+  // 50 columns 28 and 37 (36 and 38, 63 and 59).
   if (dtype != COMET_F64 && c.src[0].A.nnz >= 64 * c.src[0].A.rows) return false;
   return c.R >= 4 && c.src[0].A.nnz >= (plain ? 100000 : c.mode == kLayer ? 250000 : 500000);
 }

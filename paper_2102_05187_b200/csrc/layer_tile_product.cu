@@ -480,10 +480,16 @@ template <class T> comet_status_t product_typed(Context *ctx, const GatherCall &
 
 }  // namespace
 
-// Entries x columns from which a product is one for tiles.
-static double least_work() {
-  const char *e = getenv("COMET_LAYER_TILE_WORK");
-  return e ? atof(e) : 40e6;
+// Tiles do the work of all cells, entries or not, in steps of 64 columns, behind some 25 us of listing; a worker per row does the entries' alone, at about 1.1 us
+// a million of entries x columns. So tiles pay from 40 million of those on, where there is at least one for every cell, and 20 columns. Measured, tiles and
+// rows, bf16, us: 10 % of 1728^2, 64 columns (19 M) 36 and 21, of 2496^2 (39 M) 39 and 45, of 3520^2 (77 M) 44 and 61; 40 %, 256 columns 36 and 34 at
+// 15 M, 44 and 69 at 69 M; 2 % of 8192^2, 32 columns (0.6 a cell) 67 and 44, 48 columns (1.0) 68 and 75; 10 % of 8192^2, 16 columns 97
+// and 82, 24 columns 99 and 143; 30 % of 4096^2, 16 columns 68 and 53, 24 columns 67 and 92; 1/64 of 4096^2, 512 columns 52 and 112.
+// Below 1/64 of the cells the lists outgrow the entries.
+static bool enough_work(double nnz, double cells, int64_t R) {
+  const double work = nnz * (double)R;
+  if (const char *e = getenv("COMET_LAYER_TILE_WORK")) return work >= atof(e);
+  return work >= 40e6 && work >= cells && R >= 20;
 }
 
 bool tile_product_fits(int dtype, const GatherCall &c) {
@@ -497,7 +503,7 @@ bool tile_product_fits(int dtype, const GatherCall &c) {
     nnz += (double)g.A.nnz;
     cells += (double)g.A.rows * (double)g.A.cols;
   }
-  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && nnz * (double)c.R >= least_work();
+  return cells > 0 && nnz < 2147480000.0 && nnz * 64 >= cells && enough_work(nnz, cells, c.R);
 }
 
 comet_status_t tile_product(Context *ctx, int dtype, const GatherCall &c, const TileList *lists, cudaStream_t s) {

@@ -193,3 +193,16 @@ def test_one_copy_of_a_gradient_for_both_of_its_products(cuda_device, any_work):
     assert_within(dval, want, stored(dt, want, 71 * u_of(dt) * N), "dval")
     want, N = m.dense.t() @ dC64, m.dense.abs().t() @ dC64.abs()
     assert_within(dB, want, stored(dt, want, z_bound(dt, m.tallest, N, want)), "dB")
+
+
+@pytest.mark.parametrize("rows,cols,density,R,launches", [
+    (2500, 8000, 0.2, 19, 1), (2500, 8000, 0.2, 20, COPY + LISTS + PRODUCT), (2700, 16_000, 0.02, 48, 1), (2700, 16_000, 0.02, 56, LISTS + PRODUCT),
+    (2500, 20_000, 0.02, 48, 4),                           # by rows as well: three launches for rows of more than 16,384 entries, which it could have
+])
+def test_where_tiles_begin(cuda_device, rows, cols, density, R, launches):
+    """With enough work: from 20 columns on, and as many products as cells."""
+    rng = np.random.default_rng(R)
+    dt = torch.bfloat16
+    m = Matrix(random_mask(rows, cols, density, rng), dt, rng, scale=(cols * density) ** -0.5)
+    with Launches(launches):
+        check_epilogue(m, dt, R, "gelu", "rows", True, True, rng)
