@@ -206,3 +206,40 @@ def test_where_tiles_begin(cuda_device, rows, cols, density, R, launches):
     m = Matrix(random_mask(rows, cols, density, rng), dt, rng, scale=(cols * density) ** -0.5)
     with Launches(launches):
         check_epilogue(m, dt, R, "gelu", "rows", True, True, rng)
+
+
+IN_PLACE = {  # rows, cols, density, type, columns, columns between rows: each form that adds a residual
+    "tile": (200, 1000, 0.3, "bf16", 64, 0), "tile, unaligned": (200, 1000, 0.3, "f16", 61, 2), "split": (130, 8300, 0.1, "bf16", 256, 0),
+    "split, unaligned": (130, 4200, 0.3, "bf16", 121, 1), "panel": (3000, 900, 0.3, "f32", 3, 1), "panels": (450, 12_801, 0.5, "f64", 2, 0),
+    "rows": (300, 700, 0.4, "f32", 50, 0), "huge row": (40, 40_000, 0.02, "f16", 12, 4), "short rows, 16 bits": (24_000, 1800, 0.0145, "bf16", 20, 0),
+    "short rows, kept": (24_000, 1800, 0.0145, "f64", 6, 1),
+}
+
+
+@pytest.mark.parametrize("kind", list(IN_PLACE))
+def test_residual_in_place_in_every_form(cuda_device, any_work, kind):
+    """C += .. where the residual is C itself, its padding left alone, with and without the pre-activation kept; the same bits as with a residual of its own, and again on
+    another stream."""
+    rows, cols, density, dtype, R, pad = IN_PLACE[kind]
+    dt = TYPES[dtype]
+    rng = np.random.default_rng(R)
+    mask = random_mask(rows, cols, density, rng)
+    if kind == "huge row":
+        mask[3, :30_000] = True
+    m = Matrix(mask, dt, rng, scale=(cols * density) ** -0.5)
+    (B, _), (r, _) = values((cols, R), dt, rng), values((rows, R), dt, rng)
+    B = B.cuda()
+    for keep in (False, True):
+        pre = torch.empty(rows, R, dtype=dt, device="cuda") if keep else None
+        want = comet.spmm_epilogue(m.t, B, act=ACTS["gelu_tanh"], residual=place(r, pad), preact=pre)
+        kept = pre.clone() if keep else None
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        for s in (torch.cuda.current_stream(), stream):
+            with torch.cuda.stream(s):
+                out = place(r, pad, fill=7.0)
+                comet.spmm_epilogue(m.t, B, act=ACTS["gelu_tanh"], residual=out, preact=pre, out=out)
+                torch.cuda.synchronize()
+                assert torch.equal(out, want)
+                untouched(out, pad)
+                assert not keep or torch.equal(pre, kept)
