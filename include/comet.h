@@ -55,8 +55,8 @@ extern "C" {
 
 typedef enum { COMET_D = 0, COMET_CU = 1, COMET_CN = 2, COMET_S = 3 } comet_attr_t;
 /* COMET_BF16 / COMET_F16: values of the layer operators (comet_spmm_epilogue and what follows it below) only; every other call returns
- * COMET_ERR_UNSUPPORTED_FORMAT for them. Such a tensor is described by the caller: the level arrays of a packed tensor and a value array
- * of its own. COMET_I32: what comet_transpose_symbolic leaves in val. */
+ * COMET_ERR_UNSUPPORTED_FORMAT for them (comet_validate, which does not look at values, takes them). Such a tensor is described by the
+ * caller: the level arrays of a packed tensor and a value array of its own. COMET_I32: what comet_transpose_symbolic leaves in val. */
 typedef enum { COMET_F64 = 0, COMET_F32 = 1, COMET_BF16 = 2, COMET_F16 = 3, COMET_I32 = 4 } comet_dtype_t;
 
 typedef enum {
@@ -341,8 +341,8 @@ comet_status_t comet_elementwise_mul(comet_handle_t handle, const comet_sptensor
  *     columns and more, enough work), sampled products from 1/128 and one entry x column per cell on; short rows go through the kernels of
  *     comet_spmm, 16-bit operands as fp32 copies.
  *   - Temporary memory: the lists of the tensor-core product take 4 bytes per entry and 8 per row and block of 64 columns of A (one block more,
- *     and rounded up to 8 blocks: at 1/64 of the cells 12 bytes per entry in wide matrices, 68 in one of 64 columns); operands whose rows do not start on 16 bytes are copied where
- *     that pays; the copies in fp32 take 4 bytes per value of A, B and C. A product that gets none of this from the allocator falls back to
+ *     and rounded up to 8 blocks: at 1/64 of the cells 12 bytes per entry in wide matrices, 68 in one of 64 columns); operands whose rows do
+ *     not start on 16 bytes are copied where that pays; the copies in fp32 take 4 bytes per value of A, B and C. A product that gets none of this from the allocator falls back to
  *     kernels that need no memory. COMET_ERR_ALLOC is left for what there is no form without: row boundaries, the values of a
  *     transposed matrix in its order, dZ, column sums.
  */
@@ -370,7 +370,8 @@ comet_status_t comet_spmm_epilogue(comet_handle_t handle, const comet_sptensor_t
  *   dB       = A^T dZ                                      columns of A x R, leading dimension lddb, every row written
  *   dbias    = sums of dZ along its rows or columns, by bias_along (read only where dbias is given)
  * each only where its pointer is not NULL; the residual's gradient is dC. At: comet_transpose_symbolic(A), needed for dB alone (NULL otherwise);
- * A's values may have changed since. B is needed for dval alone. dZ is held in the operands' type (rows x R of temporary memory). */
+ * A's values may have changed since. B is needed for dval alone. dZ is held in the operands' type (rows x R of temporary memory): dval and dB
+ * of 16-bit operands carry its rounding beside their own (about 1.4 times the error of one), and of COMET_F16 no dZ beyond 65,504; dbias does not. */
 comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, const comet_sptensor_t *A, const comet_sptensor_t *At, const void *B,
                                             int64_t R, int64_t ldb, int32_t act, const void *preact, int64_t ldz, const void *dC, int64_t lddc,
                                             int32_t bias_along, void *dbias, void *dval, void *dB, int64_t lddb, void *stream);

@@ -441,6 +441,10 @@ extern "C" comet_status_t comet_transpose_symbolic(comet_handle_t handle, const 
   return st;
 }
 
+// dZ is held in the operands' type, so that both of its products run as the forward one does, in 16 bits on the tensor cores. A 16-bit gradient is thereby rounded
+// twice, as dZ and when it is stored: in bf16 it is 2.3e-3 of its norm off the result in 64 bits, where one rounding leaves 1.7e-3 (fp16: an eighth of both, and a dZ
+// beyond 65,504 is infinite). The bias gradients are sums from before that rounding. Two 16-bit terms for dZ would take twice the products: sampled, 8192 x
+// 2048 at 20 % and 512 columns 46 us instead of 36, the sum of two products about 310 instead of 158; a graph of 3.2 M entries, 64 columns 472 instead of 247.
 extern "C" comet_status_t comet_spmm_epilogue_backward(comet_handle_t handle, const comet_sptensor_t *A, const comet_sptensor_t *At, const void *B,
                                                        int64_t R, int64_t ldb, int32_t act, const void *preact, int64_t ldz, const void *dC,
                                                        int64_t lddc, int32_t bias_along, void *dbias, void *dval, void *dB, int64_t lddb, void *stream) {

@@ -4,8 +4,8 @@
 //
 //   starts  starts[i][b] = the first entry of row i at or beyond block b of k: a warp walks a row, and its lanes write where blocks change
 //   shifts  the words of tile (t, b) begin behind those of the strip's rows in earlier blocks: bases[t][b] = pos[first row] + sum over the
-//           strip's 128 rows of starts[i][b] - pos[i], no scan over tiles; within it row by row. starts[i][b] becomes what has to be added to an
-//           entry's number to get its word's
+//           strip's 128 rows of starts[i][b] - pos[i], no scan over tiles; within it row by row. What has to be added to an entry's
+//           number to get its word's goes beside the starts, in the second half of the row's words
 //   words   a warp walks a row again, 32 entries at a time, and every lane puts its word where it belongs
 //
 // (Spreading rows' pieces in the product kernel, 8 lanes to a row, took 1,230 cycles for a block of 820 entries, 2,900 instructions, where the block's
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kListThreads) tile_shifts_kernel(const ListArg
   }
   front[warp][lane] = before;
   words[warp][lane] = sum;
-  __syncthreads();                                         // (every start is read before any is replaced; the next 32 blocks' first ones are another CTA's: below)
+  __syncthreads();
   int32_t base = __ldg(s.pos + row0);
   for (int w = 0; w < kListWarps; ++w) base += front[w][lane];
   if (warp == 0 && have) s.bases[(int64_t)blockIdx.x * (a.k_blocks + 1) + b] = base;
