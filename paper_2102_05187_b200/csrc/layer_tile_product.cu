@@ -179,7 +179,8 @@ template <int kWords> struct Spreader {
       if (at + 128 * j < end) w[j] = __ldg(words + at + 128 * j);
   }
   __device__ __forceinline__ void put(uint32_t tile, uint32_t word) const {
-    asm volatile("st.shared.u16 [%0], %1;" ::"r"(tile + (word >> 16)), "h"((uint16_t)word) : "memory");
+    // (Inside the tile whatever the word: a descriptor that was not validated may leave words unwritten.)
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(tile + (word >> 16 & (uint32_t)(kATile - 2))), "h"((uint16_t)word) : "memory");
   }
   __device__ __forceinline__ void spread(uint32_t tile) const {
 #pragma unroll
